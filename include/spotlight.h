@@ -37,6 +37,9 @@ extern "C" {
 typedef struct spotlight_ctx spotlight_ctx; /* opaque; owns only its workspace and timing events */
 
 enum { SPOTLIGHT_F32 = 0, SPOTLIGHT_BF16 = 1 };
+/* Code types of a cache held in 8 bits: floats of 4 exponent and 3 fraction bits (no infinity, largest
+ * 448), and signed integers (-127 .. 127). */
+enum { SPOTLIGHT_E4M3 = 2, SPOTLIGHT_I8 = 3 };
 
 enum {
     SPOTLIGHT_OK = 0,
@@ -53,7 +56,8 @@ enum {
     SPOTLIGHT_STAGE_HASH_QUERY = 1, /* hash + pack of the query vectors                          */
     SPOTLIGHT_STAGE_SCORE = 2,      /* Hamming distances, histograms, candidate lists            */
     SPOTLIGHT_STAGE_SELECT = 3,     /* threshold, offsets, ordered output of the selected tokens */
-    SPOTLIGHT_STAGE_ATTEND = 4,     /* gather + softmax attention over a split of the rows       */
+    SPOTLIGHT_STAGE_ATTEND = 4,     /* gather + softmax attention over a split of the rows (also
+                                       over all rows of an 8-bit cache)                          */
     SPOTLIGHT_STAGE_MERGE = 5,      /* merge of the splits' partial results; where one workgroup has a
                                        whole head it is part of ATTEND: counted, with no time of its own */
     SPOTLIGHT_STAGE_STEP_SMALL = 6, /* the whole decode step of a short context, as one kernel   */
@@ -114,7 +118,8 @@ size_t spotlight_workspace_bytes(const spotlight_config *cfg);
  * success.  The workspace holds the query codes, per-block distance histograms and candidate
  * lists (about one byte per (query head, token)), the partial attention results, a bit per key and
  * norms of the hash weights for bulk hashing (a second copy of bfloat16 weights that do not fit into
- * LDS), and room for one copy of the hash weights (spotlight_prepack_weights). */
+ * LDS), room for one copy of the hash weights (spotlight_prepack_weights), and for the partial results of
+ * attention over the whole of an 8-bit cache (8.1 MiB, less for short caches). */
 int spotlight_create(spotlight_ctx **out, const spotlight_config *cfg);
 
 /* Waits for the stream, frees the workspace and the context.  NULL is accepted. */
@@ -272,12 +277,110 @@ int spotlight_decode_step_noalloc(const spotlight_config *cfg, const void *q, co
                                   int32_t *out_idx, float *out);
 
 /*
+ * The key-value cache in 8 bits: half the bytes of a bfloat16 cache, in memory and on every read.
+ *
+ * A row of K or V is held as 128 codes, and every block of block_tokens rows of a head has one scale
+ * for K and one for V: value = code * scale.  Scales are powers of two, so the only rounding is that
+ * of the codes:  scale = 2^e with e the smallest integer, at least -126, for which no finite value of
+ * the block exceeds 448 * 2^e (E4M3) or 127 * 2^e (I8) in magnitude, and code = value / scale rounded
+ * to nearest, ties to even.  An infinity or a NaN becomes NaN: its own code in E4M3; integers have
+ * none, so there the block's scale becomes NaN until the block is written anew from its first row.
+ * The calls that read a cache take positive powers of two (and NaN) as its scales.
+ */
+typedef struct {
+    void *k, *v;              /* [B, Hkv, Nmax, d] codes, aligned to 16 bytes                            */
+    float *k_scale, *v_scale; /* [B, Hkv, ceil(Nmax / block_tokens)]                                     */
+    int32_t code_type;        /* SPOTLIGHT_E4M3 or SPOTLIGHT_I8                                          */
+    int32_t block_tokens;     /* tokens that share a scale: 16, 32, 64 or 128                            */
+} spotlight_cache;
+
+/*
+ * Quantises new rows of K and V and writes them into the cache: the rows of a prompt, or the new token
+ * of a decode step.  Entry b's rows are start_b .. start_b + count_b - 1 of the cache, with
+ * start_b = t0 + first[b] and count_b = count[b]; first NULL means 0, count NULL means n_new.  The
+ * arrays are device memory, so that a captured graph can be replayed with other positions; count[b]
+ * is taken into 0 .. n_new, and rows that fall outside 0 .. Nmax-1 are left out.
+ *
+ * Rows before start_b in the block of row start_b keep their values: that block's scale is the larger of
+ * the one it has and the one that the new rows need, and if that is not the one it has, the codes of those
+ * rows are rounded to it once more.  (A scale never shrinks until its block is written anew from the first row
+ * on.)  start_b + count_b is the cache's length from then on: the codes of rows behind stay as
+ * they are, but those in the last block no longer have a scale of their own.
+ *
+ *   K, V   [B, Hkv, n_new, d]   kv_dtype
+ *   first  [B]                  int32, device, or NULL
+ *   count  [B]                  int32, device, or NULL
+ * Errors: INVALID_ARG for a bad cache, t0 or n_new outside 0 .. Nmax, or (first NULL) t0 + n_new > Nmax.
+ */
+int spotlight_cache_write(spotlight_ctx *ctx, const spotlight_cache *cache, const void *K, const void *V, int64_t t0,
+                          int64_t n_new, const int32_t *first, const int32_t *count);
+
+/*
+ * Reads rows back: entry b's rows t0 + first[b] .. + n - 1 as code * scale, exact in either kv_dtype (a value
+ * above the type's largest becomes infinite).  Rows outside 0 .. Nmax-1 become zeros.
+ *   K, V   [B, Hkv, n, d]   kv_dtype, written; either may be NULL
+ *   first  [B]              int32, device, or NULL (0)
+ * Errors: INVALID_ARG for a bad cache, both outputs NULL, t0 or n outside 0 .. Nmax, or (first NULL) t0 + n > Nmax.
+ */
+int spotlight_cache_read(spotlight_ctx *ctx, const spotlight_cache *cache, int64_t t0, int64_t n, const int32_t *first,
+                         void *K, void *V);
+
+/*
+ * spotlight_sparse_decode over an 8-bit cache: the same arguments, the same result from the values that the
+ * codes stand for, with binary32 accumulation.  A query head whose list names no row of the cache gets
+ * zeros.
+ */
+int spotlight_sparse_decode_cache(spotlight_ctx *ctx, const void *q, const spotlight_cache *cache, const int32_t *idx,
+                                  int32_t k, float scale, float *out);
+
+/*
+ * Attention over ALL rows of an 8-bit cache (Eq. 1), for layers that keep full attention: of the last n_q
+ * tokens of each sequence, whose rows are in the cache already.  Entry b has len_b = lens[b] tokens (lens NULL:
+ * n_tokens; values are taken into 0 .. n_tokens), and its query i is token len_b - n_q + i, which attends the
+ * tokens up to itself.  A query without a token to attend (len_b + i < n_q) gets zeros.  Rows from len_b on
+ * are not read.
+ *   q     [B, Hq, n_q, d]  kv_dtype
+ *   lens  [B]              int32, device, or NULL
+ *   out   [B, Hq, n_q, d]  float32
+ * The call enqueues two kernels, or one where the keys need no splitting, and nothing else.
+ * Errors: INVALID_ARG for a bad cache or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax; UNSUPPORTED if more than
+ * 2^25 tokens would have to be split further than the workspace allows for (over 16384 / ceil(n_tokens / 2^25) rows of q).
+ */
+int spotlight_dense_decode_cache(spotlight_ctx *ctx, const void *q, const spotlight_cache *cache, int64_t n_tokens,
+                                 int32_t n_q, const int32_t *lens, float scale, float *out);
+
+/*
+ * spotlight_hash_keys for rows that lie by themselves, as they do beside an 8-bit cache:
+ *   K      [B, Hkv, n_new, d]    kv_dtype
+ *   codes  [B, Hkv, Nmax, W]     uint32   rows t0 .. t0+n_new-1 written
+ * Errors: those of spotlight_hash_keys.
+ */
+int spotlight_hash_rows(spotlight_ctx *ctx, const void *K, const spotlight_hash_weights *w, int64_t t0, int64_t n_new,
+                        uint32_t *codes);
+
+/*
+ * spotlight_decode_step over an 8-bit cache: the new token's key is hashed (as it is, before it is quantised) and its key and
+ * value written into row n_tokens-1 of the cache, and attention runs over the selected rows of the cache.  It equals
+ * spotlight_hash_rows + spotlight_cache_write (t0 = n_tokens-1, n_new = 1) + spotlight_retrieve_topk (or, with
+ * forced tokens, that part of spotlight_decode_step) + spotlight_sparse_decode_cache.
+ *   q      [B, Hq, d]         kv_dtype
+ *   K, V   [B, Hkv, 1, d]     kv_dtype   the new token's rows
+ *   codes, out_idx, out       as for spotlight_decode_step
+ * Six kernels at most and nothing else, so the call can be captured into a HIP graph.
+ * Errors: those of spotlight_decode_step; INVALID_ARG for a bad cache.
+ */
+int spotlight_decode_step_cache(spotlight_ctx *ctx, const void *q, const void *K, const void *V, const spotlight_cache *cache,
+                                const spotlight_hash_weights *w, uint32_t *codes, int64_t n_tokens, int32_t k,
+                                int32_t n_sink, int32_t n_local, float scale, int32_t *out_idx, float *out);
+
+/*
  * Stage timing for benchmarks.  While enabled, every kernel launch carries two HIP events that are
  * stamped when the kernel starts and when it ends.  spotlight_profile_read waits for the stream,
  * adds the elapsed times of the launches recorded since the last read to the per-stage totals and
  * returns the totals for `stage` (milliseconds, number of launches; an ATTEND launch that has whole heads
  * adds one to MERGE as well, so that both stages count the calls, and a bulk hash of several launches
  * counts as one, with the time of all of them).  Do not capture into a HIP graph while it is enabled.
+ * Writes into an 8-bit cache and reads from it have no stage and are not timed, like the packing of weights.
  * spotlight_profile_enable(ctx, 0) stops recording and clears the totals.  At most 8192 launches are
  * recorded between two reads; later ones are not timed.
  */

@@ -15,6 +15,7 @@ import torch
 from . import build as _build
 
 F32, BF16 = 0, 1
+E4M3, I8 = 2, 3
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP, ERR_TOO_LARGE = 0, -1, -2, -3, -4, -5
 NOALLOC_SCRATCH_BYTES = 32 << 20
 STAGES = ("hash_keys", "hash_query", "score", "select", "attend", "merge", "step_small")
@@ -25,7 +26,8 @@ SYMBOLS = (
     "spotlight_set_stream", "spotlight_strerror", "spotlight_hash_keys", "spotlight_retrieve_topk",
     "spotlight_sparse_decode", "spotlight_decode_step", "spotlight_prepack_weights", "spotlight_profile_enable",
     "spotlight_profile_read", "spotlight_build_id", "spotlight_set_option", "spotlight_bulk_hash_audit_read",
-    "spotlight_decode_step_noalloc",
+    "spotlight_decode_step_noalloc", "spotlight_cache_write", "spotlight_cache_read", "spotlight_sparse_decode_cache",
+    "spotlight_dense_decode_cache", "spotlight_hash_rows", "spotlight_decode_step_cache",
 )
 OPT_BULK_HASH_MATRIX_CORES, OPT_BULK_HASH_AUDIT, OPT_STEP_SINGLE_LAUNCH = 0, 1, 2
 
@@ -40,6 +42,11 @@ class Config(C.Structure):
 
 class HashWeights(C.Structure):
     _fields_ = [("w1", C.c_void_p), ("b1", C.c_void_p), ("w2", C.c_void_p)]
+
+
+class CacheArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("code_type", C.c_int32), ("block_tokens", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -65,6 +72,14 @@ def _load() -> C.CDLL:
                                           C.c_float, vp, vp]
     lib.spotlight_decode_step_noalloc.argtypes = [C.POINTER(Config), vp, vp, vp, C.POINTER(HashWeights), vp, i64, i32,
                                                   i32, i32, C.c_float, vp, vp]
+    cache = C.POINTER(CacheArgs)
+    lib.spotlight_cache_write.argtypes = [vp, cache, vp, vp, i64, i64, vp, vp]
+    lib.spotlight_cache_read.argtypes = [vp, cache, i64, i64, vp, vp, vp]
+    lib.spotlight_sparse_decode_cache.argtypes = [vp, vp, cache, vp, i32, C.c_float, vp]
+    lib.spotlight_dense_decode_cache.argtypes = [vp, vp, cache, i64, i32, vp, C.c_float, vp]
+    lib.spotlight_hash_rows.argtypes = [vp, vp, C.POINTER(HashWeights), i64, i64, vp]
+    lib.spotlight_decode_step_cache.argtypes = [vp, vp, vp, vp, cache, C.POINTER(HashWeights), vp, i64, i32, i32, i32,
+                                                C.c_float, vp, vp]
     lib.spotlight_prepack_weights.argtypes = [vp, C.POINTER(HashWeights)]
     lib.spotlight_profile_enable.argtypes = [vp, C.c_int]
     lib.spotlight_profile_read.argtypes = [vp, C.c_int, C.POINTER(C.c_double), C.POINTER(i64)]
@@ -90,6 +105,30 @@ def _raw_stream(index: int) -> int:
     Stream object (1.2 us a call)."""
     get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return get(index) if get is not None else torch.cuda.current_stream(index).cuda_stream
+
+
+_CODE_TYPES = {torch.float8_e4m3fn: E4M3, torch.int8: I8}
+
+
+class Cache:
+    """A key-value cache held in 8 bits: codes k, v [B, Hkv, Nmax, d] (torch.float8_e4m3fn or torch.int8)
+    and k_scale, v_scale [B, Hkv, ceil(Nmax / block_tokens)] (float32 powers of two); a value is
+    code * scale.  Spotlight.new_cache makes an empty one."""
+
+    def __init__(self, k, v, k_scale, v_scale, block_tokens: int):
+        if block_tokens not in (16, 32, 64, 128):
+            raise ValueError(f"block_tokens: want 16, 32, 64 or 128, got {block_tokens}")
+        if k.dtype not in _CODE_TYPES:
+            raise ValueError(f"k: want codes in torch.float8_e4m3fn or torch.int8, got {k.dtype}")
+        if k.dim() != 4:
+            raise ValueError("k: want [B, Hkv, Nmax, d]")
+        scales = (*k.shape[:2], -(-k.shape[2] // block_tokens))
+        for name, t, shape, dtype in (("k", k, k.shape, k.dtype), ("v", v, k.shape, k.dtype),
+                                      ("k_scale", k_scale, scales, torch.float32), ("v_scale", v_scale, scales, torch.float32)):
+            if t.dtype is not dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"{name}: want contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
+        self._args = CacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _CODE_TYPES[k.dtype], block_tokens)
 
 
 def _dtype_code(t: torch.dtype) -> int:
@@ -286,6 +325,130 @@ class Spotlight:
             raise SpotlightError(rc, "spotlight_decode_step")
         return out_idx, out
 
+    # ------------------------------------------------------------------ the cache in 8 bits
+    def new_cache(self, dtype=torch.float8_e4m3fn, block_tokens: int = 64) -> Cache:
+        """An empty 8-bit cache of this shape (zeros)."""
+        if dtype not in _CODE_TYPES:
+            raise ValueError(f"want torch.float8_e4m3fn or torch.int8, got {dtype}")
+        k, v = (torch.zeros(self._kv_shape, dtype=torch.uint8, device=self.device).view(dtype) for _ in range(2))
+        blocks = -(-self.Nmax // block_tokens) if block_tokens in (16, 32, 64, 128) else 0
+        ks, vs = (torch.ones(self.B, self.Hkv, blocks, dtype=torch.float32, device=self.device) for _ in range(2))
+        return Cache(k, v, ks, vs, block_tokens)
+
+    def _cache(self, cache: Cache):
+        if not isinstance(cache, Cache):
+            raise TypeError("cache: want a Cache")
+        if cache.k.shape != self._kv_shape or cache.k.device != self.device:
+            raise ValueError(f"cache: want {self._kv_shape} on {self.device}, got {tuple(cache.k.shape)} on {cache.k.device}")
+        return C.byref(cache._args)
+
+    def _per_entry(self, t, name):
+        return None if t is None else self._chk(t, (self.B,), torch.int32, name)
+
+    def cache_write(self, cache: Cache, K, V, t0: int = 0, first=None, count=None):
+        """Quantise the rows K, V [B, Hkv, n, d] into the cache, from row t0 + first[b] on, count[b] of them."""
+        self._sync_stream()
+        if K.dim() != 4:
+            raise ValueError("K: want [B, Hkv, n, d]")
+        n = K.shape[2]
+        shape = (self.B, self.Hkv, n, self.d)
+        rc = lib.spotlight_cache_write(self._h, self._cache(cache), self._chk(K, shape, self.kv_dtype, "K"),
+                                       self._chk(V, shape, self.kv_dtype, "V"), t0, n, self._per_entry(first, "first"),
+                                       self._per_entry(count, "count"))
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_cache_write")
+        return cache
+
+    def cache_read(self, cache: Cache, n: int, t0: int = 0, first=None, K=None, V=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Rows t0 + first[b] .. + n - 1 of the cache as K, V [B, Hkv, n, d] in kv_dtype."""
+        self._sync_stream()
+        shape = (self.B, self.Hkv, n, self.d)
+        if K is None:
+            K = torch.empty(shape, dtype=self.kv_dtype, device=self.device)
+        if V is None:
+            V = torch.empty(shape, dtype=self.kv_dtype, device=self.device)
+        rc = lib.spotlight_cache_read(self._h, self._cache(cache), t0, n, self._per_entry(first, "first"),
+                                      self._chk(K, shape, self.kv_dtype, "K"), self._chk(V, shape, self.kv_dtype, "V"))
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_cache_read")
+        return K, V
+
+    def sparse_decode_cache(self, q, cache: Cache, idx, scale: Optional[float] = None, out=None):
+        self._sync_stream()
+        qp = self._chk(q, self._q_shape, self.kv_dtype, "q")
+        if idx.dim() != 3:
+            raise ValueError("idx: want [B, Hq, k]")
+        k = idx.shape[-1]
+        ip = self._chk(idx, (self.B, self.Hq, k), torch.int32, "idx")
+        if out is None:
+            out = torch.empty(self._out_shape, dtype=torch.float32, device=self.device)
+        op = self._chk(out, self._out_shape, torch.float32, "out")
+        if scale is None:
+            scale = 1.0 / math.sqrt(self.d)
+        rc = lib.spotlight_sparse_decode_cache(self._h, qp, self._cache(cache), ip, k, float(scale), op)
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_sparse_decode_cache")
+        return out
+
+    def dense_decode_cache(self, q, cache: Cache, n_tokens: int, lens=None, scale: Optional[float] = None, out=None):
+        """Attention of the last n_q tokens of each sequence, q [B, Hq, n_q, d] or [B, Hq, d] (one token), over all
+        rows of the cache up to themselves; lens [B] are the sequences' lengths (None: n_tokens)."""
+        self._sync_stream()
+        n_q = q.shape[2] if q.dim() == 4 else 1
+        shape = (self.B, self.Hq, n_q, self.d) if q.dim() == 4 else self._q_shape
+        qp = self._chk(q, shape, self.kv_dtype, "q")
+        if out is None:
+            out = torch.empty(shape, dtype=torch.float32, device=self.device)
+        op = self._chk(out, shape, torch.float32, "out")
+        if scale is None:
+            scale = 1.0 / math.sqrt(self.d)
+        rc = lib.spotlight_dense_decode_cache(self._h, qp, self._cache(cache), n_tokens, n_q, self._per_entry(lens, "lens"),
+                                              float(scale), op)
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_dense_decode_cache")
+        return out
+
+    def hash_rows(self, K, w1, b1, w2, t0: int, codes):
+        """hash_keys for rows K [B, Hkv, n, d] that lie by themselves: rows t0 .. t0+n-1 of codes."""
+        self._sync_stream()
+        if K.dim() != 4:
+            raise ValueError("K: want [B, Hkv, n, d]")
+        n = K.shape[2]
+        kp = self._chk(K, (self.B, self.Hkv, n, self.d), self.kv_dtype, "K")
+        cp = self._chk(codes, self._codes_shape, torch.int32, "codes")
+        w = self._weights(w1, b1, w2)
+        rc = lib.spotlight_hash_rows(self._h, kp, C.byref(w), t0, n, cp)
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_hash_rows")
+        return codes
+
+    def decode_step_cache(self, q, K, V, cache: Cache, w1, b1, w2, codes, n_tokens: int, k: int, n_sink: int = 0,
+                          n_local: int = 0, scale: Optional[float] = None, out_idx=None, out=None):
+        """decode_step over an 8-bit cache: K, V [B, Hkv, 1, d] are the new token's rows, written into row
+        n_tokens-1 of the cache.  Returns (idx, out)."""
+        self._sync_stream()
+        qp = self._chk(q, self._q_shape, self.kv_dtype, "q")
+        shape = (self.B, self.Hkv, 1, self.d)
+        kp = self._chk(K, shape, self.kv_dtype, "K")
+        vp = self._chk(V, shape, self.kv_dtype, "V")
+        cp = self._chk(codes, self._codes_shape, torch.int32, "codes")
+        w = self._weights(w1, b1, w2)
+        if not (isinstance(k, int) and isinstance(n_tokens, int) and isinstance(n_sink, int) and isinstance(n_local, int)):
+            raise TypeError("k, n_tokens, n_sink and n_local are ints")
+        if out_idx is None:
+            out_idx = torch.empty(self.B, self.Hq, max(k, 0), dtype=torch.int32, device=self.device)
+        ip = self._chk(out_idx, (self.B, self.Hq, k), torch.int32, "out_idx")
+        if out is None:
+            out = torch.empty(self._out_shape, dtype=torch.float32, device=self.device)
+        op = self._chk(out, self._out_shape, torch.float32, "out")
+        if scale is None:
+            scale = 1.0 / math.sqrt(self.d)
+        rc = lib.spotlight_decode_step_cache(self._h, qp, kp, vp, self._cache(cache), C.byref(w), cp, n_tokens, k, n_sink,
+                                             n_local, float(scale), ip, op)
+        if rc != OK:
+            raise SpotlightError(rc, "spotlight_decode_step_cache")
+        return out_idx, out
+
     # ------------------------------------------------------------------ stage timing
     def profile_enable(self, on: bool = True):
         rc = lib.spotlight_profile_enable(self._h, 1 if on else 0)
@@ -335,3 +498,27 @@ def spotlight_prepack_weights(ctx: Spotlight, w1=None, b1=None, w2=None):
 
 def spotlight_decode_step(ctx: Spotlight, q, K, V, w1, b1, w2, codes, n_tokens, k, n_sink=0, n_local=0, **kw):
     return ctx.decode_step(q, K, V, w1, b1, w2, codes, n_tokens, k, n_sink, n_local, **kw)
+
+
+def spotlight_cache_write(ctx: Spotlight, cache: Cache, K, V, t0=0, first=None, count=None):
+    return ctx.cache_write(cache, K, V, t0, first, count)
+
+
+def spotlight_cache_read(ctx: Spotlight, cache: Cache, n, t0=0, first=None, **kw):
+    return ctx.cache_read(cache, n, t0, first, **kw)
+
+
+def spotlight_sparse_decode_cache(ctx: Spotlight, q, cache: Cache, idx, scale=None, out=None):
+    return ctx.sparse_decode_cache(q, cache, idx, scale, out)
+
+
+def spotlight_dense_decode_cache(ctx: Spotlight, q, cache: Cache, n_tokens, lens=None, scale=None, out=None):
+    return ctx.dense_decode_cache(q, cache, n_tokens, lens, scale, out)
+
+
+def spotlight_hash_rows(ctx: Spotlight, K, w1, b1, w2, t0, codes):
+    return ctx.hash_rows(K, w1, b1, w2, t0, codes)
+
+
+def spotlight_decode_step_cache(ctx: Spotlight, q, K, V, cache: Cache, w1, b1, w2, codes, n_tokens, k, n_sink=0, n_local=0, **kw):
+    return ctx.decode_step_cache(q, K, V, cache, w1, b1, w2, codes, n_tokens, k, n_sink, n_local, **kw)

@@ -67,6 +67,12 @@ int make_plan(const spotlight_config* c, Plan* p)
     p->off_operands = off;  off = align_up(off + wheads * screen_operand_bytes(p->hidden, p->W), 256);
     p->off_open = off;      off = align_up(off + kheads * ((p->Nmax + 31) / 32) * 4, 256);
     p->off_open_counts = off; off = align_up(off + kheads * ((p->Nmax + 65535) / 65536) * 128, 256);
+    // Partial results of attention over the whole 8-bit cache.  Sixteen thousand rows: 256 workgroups of 64
+    // rows, or eight splits for each of 256 workgroups of eight; fewer where the cache cannot be split that far.
+    const int64_t most_rows = static_cast<int64_t>(BH) * ((p->Nmax + 127) / 128) * 8;
+    p->dense_rows = most_rows < 16384 ? most_rows : 16384;
+    p->off_dense_ml = off;  off = align_up(off + static_cast<size_t>(p->dense_rows) * 8, 256);
+    p->off_dense_acc = off; off = align_up(off + static_cast<size_t>(p->dense_rows) * kHeadDim * 4, 256);
     p->off_audit = off;     off = align_up(off + sizeof(AuditRec), 256);
     p->total_bytes = off;
     return SPOTLIGHT_OK;
@@ -100,14 +106,96 @@ int allow_dynamic_lds(spotlight_ctx* ctx, const void* kernel, size_t bytes)
     return SPOTLIGHT_OK;
 }
 
-static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 
-static int check_weights(const spotlight_ctx* ctx, const spotlight_hash_weights* w)
+int check_weights(const spotlight_ctx* ctx, const spotlight_hash_weights* w)
 {
     if (!w || !w->w1) return SPOTLIGHT_ERR_INVALID_ARG;
     if (ctx->plan.hidden > 0 && (!w->b1 || !w->w2)) return SPOTLIGHT_ERR_INVALID_ARG;
     if (misaligned(w->w1) || (ctx->plan.hidden > 0 && misaligned(w->w2))) return SPOTLIGHT_ERR_INVALID_ARG;
     return SPOTLIGHT_OK;
+}
+
+// The packed copy of the weights serves a job only if it was made from exactly these arrays.
+static void attach_packed(const spotlight_ctx* ctx, const spotlight_hash_weights* w, HashLaunch* h)
+{
+    const Plan& p = ctx->plan;
+    const bool match = ctx->packed_w1 && ctx->packed_w1 == w->w1 && ctx->packed_b1 == w->b1 && ctx->packed_w2 == w->w2;
+    h->pack_w1 = match && p.pack_w1_elems ? ctx->workspace + p.off_pack_w1 : nullptr;
+    h->pack_out = match && p.pack_out_elems ? ctx->workspace + p.off_pack_out : nullptr;
+}
+
+// The hash job of n_new key rows of every (batch, kv head), written into the code cache.
+HashLaunch key_job(const spotlight_ctx* ctx, const void* K, const spotlight_hash_weights* w, int64_t t0,
+                          int64_t n_new, uint32_t* codes)
+{
+    const Plan& p = ctx->plan;
+    HashLaunch h;
+    h.x = K;
+    h.x_dtype = p.kv_dtype;
+    h.x_head_stride = p.Nmax * kHeadDim;
+    h.x_row0 = t0;
+    h.n_rows = n_new;
+    h.n_xheads = p.B * p.Hkv;
+    h.heads_per_batch = p.Hkv;
+    h.group = 1;
+    h.w1 = w->w1;
+    h.b1 = w->b1;
+    h.w2 = w->w2;
+    h.w_dtype = p.w_dtype;
+    h.hidden = p.hidden;
+    h.L = p.L;
+    h.codes = codes;
+    h.code_head_stride = p.Nmax * p.W;
+    h.code_row0 = t0;
+    h.zero = nullptr;
+    h.zero_words = 0;
+    h.wnorm = ctx->opt[SPOTLIGHT_OPT_BULK_HASH_MATRIX_CORES] ? reinterpret_cast<float*>(ctx->workspace + p.off_wnorm) : nullptr;
+    h.audit = ctx->opt[SPOTLIGHT_OPT_BULK_HASH_AUDIT] ? reinterpret_cast<AuditRec*>(ctx->workspace + p.off_audit) : nullptr;
+    const bool two = h.wnorm && p.two_passes;
+    h.scales = two ? ctx->workspace + p.off_scales : nullptr;
+    h.operands = two ? ctx->workspace + p.off_operands : nullptr;
+    h.open = two ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_open) : nullptr;
+    h.open_stride = (p.Nmax + 31) / 32;
+    h.open_counts = two ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_open_counts) : nullptr;
+    attach_packed(ctx, w, &h);
+    return h;
+}
+
+// The hash job of the queries, written into the workspace; it also clears the heads' cumulative
+// histograms, which the score kernel adds into.
+HashLaunch query_job(const spotlight_ctx* ctx, const void* q, const spotlight_hash_weights* w)
+{
+    const Plan& p = ctx->plan;
+    HashLaunch h;
+    h.x = q;
+    h.x_dtype = p.kv_dtype;
+    h.x_head_stride = kHeadDim;
+    h.x_row0 = 0;
+    h.n_rows = 1;
+    h.n_xheads = p.B * p.Hq;
+    h.heads_per_batch = p.Hq;
+    h.group = p.G;
+    h.w1 = w->w1;
+    h.b1 = w->b1;
+    h.w2 = w->w2;
+    h.w_dtype = p.w_dtype;
+    h.hidden = p.hidden;
+    h.L = p.L;
+    h.codes = reinterpret_cast<uint32_t*>(ctx->workspace + p.off_qcode);
+    h.code_head_stride = p.W;
+    h.code_row0 = 0;
+    h.zero = reinterpret_cast<uint32_t*>(ctx->workspace + p.off_gcum);
+    h.zero_words = p.L + 2;
+    h.wnorm = nullptr;
+    h.audit = nullptr;
+    h.scales = nullptr;
+    h.operands = nullptr;
+    h.open = nullptr;
+    h.open_stride = 0;
+    h.open_counts = nullptr;
+    attach_packed(ctx, w, &h);
+    return h;
 }
 
 }  // namespace spotlight
@@ -166,6 +254,7 @@ int spotlight_create(spotlight_ctx** out, const spotlight_config* cfg)
     }
     ctx->max_lds = lds;
     ctx->n_cus = cus;
+    ctx->device = dev;
     ctx->opt[SPOTLIGHT_OPT_BULK_HASH_MATRIX_CORES] = 1;
     void* ws = nullptr;
     if (hipMalloc(&ws, plan.total_bytes) != hipSuccess) {
@@ -238,88 +327,6 @@ int spotlight_set_stream(spotlight_ctx* ctx, void* stream)
     if (!ctx) return SPOTLIGHT_ERR_INVALID_ARG;
     ctx->stream = static_cast<hipStream_t>(stream);
     return SPOTLIGHT_OK;
-}
-
-// The packed copy of the weights serves a job only if it was made from exactly these arrays.
-static void attach_packed(const spotlight_ctx* ctx, const spotlight_hash_weights* w, HashLaunch* h)
-{
-    const Plan& p = ctx->plan;
-    const bool match = ctx->packed_w1 && ctx->packed_w1 == w->w1 && ctx->packed_b1 == w->b1 && ctx->packed_w2 == w->w2;
-    h->pack_w1 = match && p.pack_w1_elems ? ctx->workspace + p.off_pack_w1 : nullptr;
-    h->pack_out = match && p.pack_out_elems ? ctx->workspace + p.off_pack_out : nullptr;
-}
-
-// The hash job of n_new key rows of every (batch, kv head), written into the code cache.
-static HashLaunch key_job(const spotlight_ctx* ctx, const void* K, const spotlight_hash_weights* w, int64_t t0,
-                          int64_t n_new, uint32_t* codes)
-{
-    const Plan& p = ctx->plan;
-    HashLaunch h;
-    h.x = K;
-    h.x_dtype = p.kv_dtype;
-    h.x_head_stride = p.Nmax * kHeadDim;
-    h.x_row0 = t0;
-    h.n_rows = n_new;
-    h.n_xheads = p.B * p.Hkv;
-    h.heads_per_batch = p.Hkv;
-    h.group = 1;
-    h.w1 = w->w1;
-    h.b1 = w->b1;
-    h.w2 = w->w2;
-    h.w_dtype = p.w_dtype;
-    h.hidden = p.hidden;
-    h.L = p.L;
-    h.codes = codes;
-    h.code_head_stride = p.Nmax * p.W;
-    h.code_row0 = t0;
-    h.zero = nullptr;
-    h.zero_words = 0;
-    h.wnorm = ctx->opt[SPOTLIGHT_OPT_BULK_HASH_MATRIX_CORES] ? reinterpret_cast<float*>(ctx->workspace + p.off_wnorm) : nullptr;
-    h.audit = ctx->opt[SPOTLIGHT_OPT_BULK_HASH_AUDIT] ? reinterpret_cast<AuditRec*>(ctx->workspace + p.off_audit) : nullptr;
-    const bool two = h.wnorm && p.two_passes;
-    h.scales = two ? ctx->workspace + p.off_scales : nullptr;
-    h.operands = two ? ctx->workspace + p.off_operands : nullptr;
-    h.open = two ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_open) : nullptr;
-    h.open_stride = (p.Nmax + 31) / 32;
-    h.open_counts = two ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_open_counts) : nullptr;
-    attach_packed(ctx, w, &h);
-    return h;
-}
-
-// The hash job of the queries, written into the workspace; it also clears the heads' cumulative
-// histograms, which the score kernel adds into.
-static HashLaunch query_job(const spotlight_ctx* ctx, const void* q, const spotlight_hash_weights* w)
-{
-    const Plan& p = ctx->plan;
-    HashLaunch h;
-    h.x = q;
-    h.x_dtype = p.kv_dtype;
-    h.x_head_stride = kHeadDim;
-    h.x_row0 = 0;
-    h.n_rows = 1;
-    h.n_xheads = p.B * p.Hq;
-    h.heads_per_batch = p.Hq;
-    h.group = p.G;
-    h.w1 = w->w1;
-    h.b1 = w->b1;
-    h.w2 = w->w2;
-    h.w_dtype = p.w_dtype;
-    h.hidden = p.hidden;
-    h.L = p.L;
-    h.codes = reinterpret_cast<uint32_t*>(ctx->workspace + p.off_qcode);
-    h.code_head_stride = p.W;
-    h.code_row0 = 0;
-    h.zero = reinterpret_cast<uint32_t*>(ctx->workspace + p.off_gcum);
-    h.zero_words = p.L + 2;
-    h.wnorm = nullptr;
-    h.audit = nullptr;
-    h.scales = nullptr;
-    h.operands = nullptr;
-    h.open = nullptr;
-    h.open_stride = 0;
-    h.open_counts = nullptr;
-    attach_packed(ctx, w, &h);
-    return h;
 }
 
 int spotlight_prepack_weights(spotlight_ctx* ctx, const spotlight_hash_weights* w)

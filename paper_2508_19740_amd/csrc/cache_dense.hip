@@ -1,0 +1,485 @@
+// Attention of the last n_q tokens of each sequence over the whole 8-bit cache.
+//
+// The rows of a key-value head are its G query heads times n_q queries, contiguous in q.  A wavefront
+// takes tiles of 16 rows and a run of keys, 32 keys a step, and needs neither LDS nor a barrier until its
+// keys are done:
+//
+//   S^T = K Q^T     v_mfma_f32_16x16x32_f16.  Lane (g, i) = (lane / 16, lane % 16) loads 32 adjacent
+//                   bytes of key i; four products take 8 of them each, and q lies in registers in the
+//                   same order.  The result leaves lane (g, i) with keys 4g .. 4g+3 of query row i.
+//   softmax         a row's maximum changes rarely: lanes compare their own scores with the last maximum,
+//                   and only where one is larger is the maximum taken over the lanes and what has been
+//                   summed rescaled.
+//   O^T += V^T P^T  The lane holds the weights just where the second operand wants them (the keys of a
+//                   product may come in any order).  The first operand wants the same keys of one
+//                   column: lane (g, i) loads 8 bytes, columns 8i .. 8i+7, of each of its eight keys, and
+//                   swaps keys for columns with byte permutes.
+//
+// Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
+//   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
+//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).
+//   p   is in [0, 1], scaled by 2^15 and split in two parts.
+//   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
+//       ratio is above 2^-20, and at most 2^-30 of the largest block's size off below.
+//
+// A row reads 256 bytes a key and key-value head, whatever G and n_q: with few rows the kernel is bound by
+// memory.  The keys are split over workgroups, and a merge joins them.
+#include "cache.h"
+
+namespace spotlight {
+using namespace cache;
+namespace {
+
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+
+constexpr int kStep = kDenseStep;       // keys of a step
+constexpr int kWaves = kDenseWaves;
+static_assert(kWaves == kThreads / 64, "wavefronts of a workgroup");
+constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^15
+constexpr float kPUp = 15.0f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+__device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d)
+{
+    return h8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// Binary16 operands from codes.
+template <typename CT> struct Operand;
+template <> struct Operand<E4M3> {
+    // eight codes of a key
+    static __device__ __forceinline__ h8 row(uint32_t lo, uint32_t hi)
+    {
+        return join(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true),
+                    __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    }
+    // four columns of the keys a and b, times a power of two: o[c] = (a[c], b[c])
+    typedef float Ratio;
+    static __device__ __forceinline__ Ratio ratio(float r) { return r; }
+    static __device__ __forceinline__ void columns(uint32_t a, uint32_t b, Ratio r, h2 (&o)[4])
+    {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const h2 x = j ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, r, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, r, false);
+            const h2 y = j ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, r, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, r, false);
+            o[2 * j] = h2{x.x, y.x};
+            o[2 * j + 1] = h2{x.y, y.y};
+        }
+    }
+};
+template <> struct Operand<I8> {
+    // 0x6400 | u is 1024 + u in binary16; u is the code with its sign bit flipped, code + 128
+    static __device__ __forceinline__ h2 pair(uint32_t biased) { return __builtin_bit_cast(h2, biased) - h2{1152.0f16, 1152.0f16}; }
+    static __device__ __forceinline__ h8 row(uint32_t lo, uint32_t hi)
+    {
+        lo ^= 0x80808080u;
+        hi ^= 0x80808080u;
+        return join(pair(__builtin_amdgcn_perm(lo, 0x64646464u, 0x00050004u)), pair(__builtin_amdgcn_perm(lo, 0x64646464u, 0x00070006u)),
+                    pair(__builtin_amdgcn_perm(hi, 0x64646464u, 0x00050004u)), pair(__builtin_amdgcn_perm(hi, 0x64646464u, 0x00070006u)));
+    }
+    struct Ratio { h2 r, bias; };
+    static __device__ __forceinline__ Ratio ratio(float r)
+    {
+        const _Float16 h = static_cast<_Float16>(r);
+        return Ratio{h2{h, h}, h2{-1152.0f16 * h, -1152.0f16 * h}};
+    }
+    static __device__ __forceinline__ void columns(uint32_t a, uint32_t b, const Ratio& r, h2 (&o)[4])
+    {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint32_t w = __builtin_amdgcn_perm(a, b, 0x0c000c04u + 0x00010001u * c) ^ 0x64806480u;
+            o[c] = __builtin_elementwise_fma(__builtin_bit_cast(h2, w), r.r, r.bias);
+        }
+    }
+};
+
+struct DenseArgs {
+    const void* q;
+    const uint8_t* k;
+    const uint8_t* v;
+    const float* k_scale;
+    const float* v_scale;
+    const int32_t* lens;
+    float2* part_ml;
+    float* part_acc;
+    float* out;
+    int64_t Nmax, blocks, n_tokens;
+    int64_t chunk;                      // keys of a split, a multiple of kStep * kWaves
+    int64_t rows;                       // rows of a key-value head: G * n_q
+    int n_q, Hkv, nsplit, shift;
+    float scale2;                       // scale * log2(e)
+};
+
+template <bool B> struct Flag { static constexpr bool value = B; };
+
+__device__ __forceinline__ float across_groups_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float across_groups_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// One row's 32 elements of a lane, scaled by 2^(13 - exponent of the row's largest) and split into QP
+// binary16 parts; returns the exponent that was taken out.
+template <typename QT, int QP>
+__device__ __forceinline__ int load_row(const QT* q, h8 (&frag)[QP][4])
+{
+    float x[32];
+    if constexpr (sizeof(QT) == 2) {
+        const uint4* s = reinterpret_cast<const uint4*>(q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 u = s[i];
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { x[8 * i + 2 * j] = __uint_as_float(w[j] << 16); x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+        }
+    } else {
+        const float4* s = reinterpret_cast<const float4*>(q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 u = s[i];
+            x[4 * i] = u.x; x[4 * i + 1] = u.y; x[4 * i + 2] = u.z; x[4 * i + 3] = u.w;
+        }
+    }
+    float most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) most = fmaxf(most, fabsf(x[i]));
+    most = across_groups_max(most);
+    const int ex = (most > 0.0f && most < INFINITY) ? ilogbf(most) : 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float y = ldexpf(x[8 * c + j], 13 - ex);
+            const _Float16 hi = static_cast<_Float16>(y);
+            frag[0][c][j] = hi;
+            if constexpr (QP == 2) frag[1][c][j] = static_cast<_Float16>(y - static_cast<float>(hi));
+        }
+    return ex - 13;
+}
+
+// MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a split.
+template <typename CT, typename QT, int MT>
+__global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
+{
+    constexpr int QP = sizeof(QT) == 2 ? 1 : 2;
+    typedef Operand<CT> Op;
+    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    __shared__ float s_acc[kWaves][16][kHeadDim + 4];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, i = lane & 15;
+    const int split = static_cast<int>(blockIdx.x % a.nsplit);
+    const int64_t r0 = static_cast<int64_t>(blockIdx.x / a.nsplit) * (16 * MT);
+    const int64_t head = blockIdx.y;
+
+    int64_t len = a.n_tokens;
+    if (a.lens) len = min(max(static_cast<int64_t>(a.lens[head / a.Hkv]), static_cast<int64_t>(0)), len);
+
+    // keys each of this lane's rows sees: those before `seen`.  Rows behind the last repeat it.
+    int64_t seen[MT], least = len, most = 0;
+    h8 qf[MT][QP][4];
+    float factor[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int64_t r = min(r0 + 16 * t + i, a.rows - 1);
+        seen[t] = max(len - a.n_q + r % a.n_q + 1, static_cast<int64_t>(0));
+        least = min(least, seen[t]);
+        most = max(most, seen[t]);
+        const int ex = load_row<QT, QP>(static_cast<const QT*>(a.q) + (head * a.rows + r) * kHeadDim + g * 32, qf[t]);
+        factor[t] = ldexpf(a.scale2, ex);
+    }
+#pragma unroll
+    for (int off = 1; off < 16; off <<= 1) {
+        least = min(least, static_cast<int64_t>(__shfl_xor(static_cast<long long>(least), off)));
+        most = max(most, static_cast<int64_t>(__shfl_xor(static_cast<long long>(most), off)));
+    }
+
+    // this wavefront's keys
+    const int64_t c0 = split * a.chunk, c1 = min(c0 + a.chunk, most);
+    const int64_t share = a.chunk / kWaves;
+    const int64_t k0 = c0 + wave * share;
+    const int n = __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(c1 - k0, static_cast<int64_t>(0)), share)));
+    const int steps = (n + kStep - 1) / kStep;
+    // the first steps, whose keys every row sees
+    const int plain_steps = __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(least - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n)) / kStep));
+    int sees[MT];                       // keys of the run that the lane's row sees
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sees[t] = static_cast<int>(min(max(seen[t] - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n)));
+
+    // Rows behind the run read as zeros: the buffer ends with it.  Offsets within it stay below 2^31 (the host
+    // bounds a split), and all of them are in the instruction's checked part.
+    const int64_t base = (head * a.Nmax + k0) * kHeadDim;
+    const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.k + base), 0, n * kHeadDim, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.v + base), 0, n * kHeadDim, 0x00020000);
+    const float* ks = a.k_scale + head * a.blocks;
+    const float* vs = a.v_scale + head * a.blocks;
+    const int64_t last_block = (k0 + (n > 0 ? n - 1 : 0)) >> a.shift;
+
+    // the largest scale of the run's values
+    float unit = 0.0f;
+    if (n > 0)
+        for (int64_t j = (k0 >> a.shift) + lane; j <= last_block; j += 64) unit = fmaxf(unit, vs[j]);
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) unit = fmaxf(unit, __shfl_xor(unit, off));
+    if (!(unit > 0.0f)) unit = 1.0f;
+    const int unit_bits = __builtin_amdgcn_readfirstlane(__float_as_int(unit)) - ((127 + kVUp) << 23);
+
+    f4 acc[MT][8];
+    float m[MT], l[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        m[t] = -INFINITY;
+        l[t] = 0.0f;
+#pragma unroll
+        for (int d = 0; d < 8; ++d) acc[t][d] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+
+    u4 kreg[2][2];
+    u2 vreg[2][4];
+    const int koff = i * kHeadDim + g * 32, voff = g * (4 * kHeadDim) + i * 8;
+    auto load_k = [&](int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + s * (kStep * kHeadDim) + (t * (16 * kHeadDim) + j * 16), 0, 0);
+    };
+    auto load_v = [&](int s) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                vreg[t][r] = __builtin_amdgcn_raw_buffer_load_b64(vr, voff + s * (kStep * kHeadDim) + (t * (16 * kHeadDim) + r * kHeadDim), 0, 0);
+    };
+
+    auto step = [&](int s, auto masked) {
+        const int64_t key = k0 + static_cast<int64_t>(s) * kStep;
+        float kscale[2];
+        typename Op::Ratio ratio[2];
+        bool nan_values = false;                                // of this step; asked only where a row sees part of it
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const int64_t blk = min((key + 16 * t) >> a.shift, last_block);
+            kscale[t] = ks[blk];
+            const float v = vs[blk];
+            const int up = __float_as_int(v) - unit_bits;       // powers of two: a difference of exponents
+            ratio[t] = Op::ratio(v != v ? v : up > 0 ? __int_as_float(up) : 0.0f);
+            if constexpr (decltype(masked)::value && !CT::kHasNaN) nan_values |= v != v;
+        }
+        if constexpr (decltype(masked)::value && CT::kHasNaN) {
+            uint32_t found = 0;                                 // bytes of 7f and ff
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) found |= (((vreg[t][r].x & 0x7f7f7f7fu) + 0x01010101u) | ((vreg[t][r].y & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u;
+            nan_values = __any(found != 0);
+        }
+        // scores
+        f4 sc[MT][2];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) sc[t][0] = sc[t][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const h8 kf = Op::row(kreg[kt][c / 2][2 * (c % 2)], kreg[kt][c / 2][2 * (c % 2) + 1]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int p = 0; p < QP; ++p) sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][kt], 0, 0, 0);
+            }
+        load_k(s + 1);
+        // softmax
+        h8 hi[MT], lo[MT];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            float x[8];
+            float top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = sc[t][e / 4][e % 4] * (factor[t] * kscale[e / 4]);
+                if constexpr (decltype(masked)::value)
+                    if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
+                top = fmaxf(top, x[e]);
+            }
+            if (__any(top > m[t])) {
+                const float mn = across_groups_max(fmaxf(m[t], top));
+                // nothing before: nothing to rescale
+                const float down = m[t] > -INFINITY ? __builtin_amdgcn_exp2f(m[t] - mn) : 0.0f;
+                l[t] *= down;
+#pragma unroll
+                for (int d = 0; d < 8; ++d) acc[t][d] *= down;
+                m[t] = mn;
+            }
+            const float base2 = (m[t] > -INFINITY ? m[t] : 0.0f) - kPUp;
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = __builtin_amdgcn_exp2f(x[e] - base2);
+                sum += x[e];
+            }
+            l[t] += sum;
+            h2 h[4], r[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                h[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x[2 * e], x[2 * e + 1]));
+                r[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x[2 * e] - static_cast<float>(h[e].x), x[2 * e + 1] - static_cast<float>(h[e].y)));
+            }
+            hi[t] = join(h[0], h[1], h[2], h[3]);
+            lo[t] = join(r[0], r[1], r[2], r[3]);
+        }
+        // weighted values: four columns of the lane at a time
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            h2 col[4][4];                       // [pair of keys][column]
+#pragma unroll
+            for (int pr = 0; pr < 4; ++pr) Op::columns(vreg[pr / 2][2 * (pr % 2)][w], vreg[pr / 2][2 * (pr % 2) + 1][w], ratio[pr / 2], col[pr]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                h8 vf = join(col[0][c], col[1][c], col[2][c], col[3][c]);
+                if constexpr (decltype(masked)::value) {
+                    // A row's weight 0 must not meet a NaN of a key that it does not see: the product is
+                    // formed without NaN, and one of "is NaN" and "sees the key" tells which sums are NaN.
+                    if (nan_values) {
+                        h8 is_nan;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const bool bad = !(vf[j] == vf[j]);
+                            is_nan[j] = bad ? 1.0f16 : 0.0f16;
+                            vf[j] = bad ? 0.0f16 : vf[j];
+                        }
+#pragma unroll
+                        for (int t = 0; t < MT; ++t) {
+                            h8 sees_key;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) sees_key[j] = s * kStep + 16 * (j / 4) + 4 * g + j % 4 < sees[t] ? 1.0f16 : 0.0f16;
+                            const f4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is_nan, sees_key, f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (hit[r] != 0.0f) acc[t][4 * w + c][r] = __builtin_nanf("");
+                        }
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[t], acc[t][4 * w + c], 0, 0, 0);
+                    acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[t], acc[t][4 * w + c], 0, 0, 0);
+                }
+            }
+        }
+        load_v(s + 1);
+    };
+    if (steps > 0) {
+        load_k(0);
+        load_v(0);
+        int s = 0;
+        for (; s < plain_steps; ++s) step(s, Flag<false>{});
+        for (; s < steps; ++s) step(s, Flag<true>{});
+    }
+
+    // the wavefronts' results, joined: lane (g, i) has columns 32g .. 32g+31 of row i
+    const float to_value = ldexpf(unit, -kVUp);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const float sum = across_groups_sum(l[t]);
+        if (t) __syncthreads();
+        if (g == 0) { s_m[wave][i] = m[t]; s_l[wave][i] = sum; }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int d = 0; d < 8; d += 4)
+                *reinterpret_cast<f4*>(&s_acc[wave][i][g * 32 + r * 8 + d]) =
+                    f4{acc[t][d][r], acc[t][d + 1][r], acc[t][d + 2][r], acc[t][d + 3][r]} * to_value;
+        __syncthreads();
+        const int64_t left = a.rows - (r0 + 16 * t);
+        for (int e = tid; e < 16 * kHeadDim && e / kHeadDim < left; e += kThreads) {
+            const int row = e / kHeadDim, col = e % kHeadDim;
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row]);
+            float o = 0.0f, lsum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (s_l[w][row] != 0.0f) {
+                    const float f = __builtin_amdgcn_exp2f(s_m[w][row] - M);
+                    o = __builtin_fmaf(f, s_acc[w][row][col], o);
+                    lsum = __builtin_fmaf(f, s_l[w][row], lsum);
+                }
+            }
+            const int64_t at = head * a.rows + r0 + 16 * t + row;
+            if (a.nsplit == 1) {
+                a.out[at * kHeadDim + col] = lsum != 0.0f ? o / lsum : 0.0f;
+            } else {
+                a.part_acc[(at * a.nsplit + split) * kHeadDim + col] = o;
+                if (col == 0) a.part_ml[at * a.nsplit + split] = make_float2(M, lsum);
+            }
+        }
+    }
+}
+
+template <typename CT, typename QT>
+void launch_mt(spotlight_ctx* ctx, StageTimer& timer, const DenseArgs& a, int mt)
+{
+    const Plan& p = ctx->plan;
+    const dim3 grid(static_cast<unsigned>((a.rows + 16 * mt - 1) / (16 * mt) * a.nsplit), static_cast<unsigned>(p.B * p.Hkv));
+    auto kern = mt == 1 ? cache_dense_kernel<CT, QT, 1> : mt == 2 ? cache_dense_kernel<CT, QT, 2> : cache_dense_kernel<CT, QT, 4>;
+    timer.launch(kern, grid, dim3(kThreads), 0, a);
+}
+
+}  // namespace
+
+int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, int64_t n_tokens, int n_q, const int32_t* lens,
+                       float scale, float* out)
+{
+    const Plan& p = ctx->plan;
+    DenseArgs a;
+    a.q = q;
+    a.k = static_cast<const uint8_t*>(c.k);
+    a.v = static_cast<const uint8_t*>(c.v);
+    a.k_scale = c.k_scale;
+    a.v_scale = c.v_scale;
+    a.lens = lens;
+    a.part_ml = reinterpret_cast<float2*>(ctx->workspace + p.off_dense_ml);
+    a.part_acc = reinterpret_cast<float*>(ctx->workspace + p.off_dense_acc);
+    a.out = out;
+    a.Nmax = p.Nmax;
+    a.blocks = (p.Nmax + c.block_tokens - 1) / c.block_tokens;
+    a.n_tokens = n_tokens;
+    a.rows = static_cast<int64_t>(p.G) * n_q;
+    a.n_q = n_q;
+    a.Hkv = p.Hkv;
+    a.shift = __builtin_ctz(static_cast<unsigned>(c.block_tokens));
+    a.scale2 = scale * kLog2e;
+
+    DenseSplit sp;
+    const int rc = split_dense(p, ctx->n_cus, n_tokens, n_q, &sp);
+    if (rc != SPOTLIGHT_OK) return rc;
+    a.chunk = sp.chunk;
+    a.nsplit = sp.nsplit;
+    {
+        StageTimer timer(ctx, SPOTLIGHT_STAGE_ATTEND);
+        if (timer.rec) timer.rec->whole = a.nsplit == 1;
+        if (p.kv_dtype == SPOTLIGHT_BF16) {
+            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, bf16_raw>(ctx, timer, a, sp.tiles);
+            else launch_mt<I8, bf16_raw>(ctx, timer, a, sp.tiles);
+        } else {
+            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, float>(ctx, timer, a, sp.tiles);
+            else launch_mt<I8, float>(ctx, timer, a, sp.tiles);
+        }
+        if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
+    }
+    if (a.nsplit == 1) return SPOTLIGHT_OK;
+    return launch_cache_merge(ctx, a.part_ml, a.part_acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, a.nsplit, out);
+}
+
+}  // namespace spotlight

@@ -44,6 +44,9 @@ struct Plan {
     size_t off_operands;   // [Hkv][screen_operand_bytes] the weights in that pass's read order
     size_t off_open;       // [B*Hkv][ceil(Nmax / 32)] rows that pass left open, a bit each
     size_t off_open_counts; // [B*Hkv][ceil(Nmax / 65536)][128 bytes] how many of each segment of a head's rows
+    size_t off_dense_ml;   // [dense_rows] {max, sum} of each split of attention over the whole 8-bit cache
+    size_t off_dense_acc;  // [dense_rows][128] weighted value sums of each split
+    int64_t dense_rows;
     size_t off_audit;      // AuditRec of the bulk hash (SPOTLIGHT_OPT_BULK_HASH_AUDIT)
     size_t total_bytes;
 };
@@ -103,6 +106,7 @@ struct spotlight_ctx {
     char* workspace;
     int max_lds;                     // bytes of LDS one workgroup may use on this device
     int n_cus;                       // compute units of this device
+    int device;                      // the device the context was made on
     int score_resident;              // score workgroups the device holds at once (0: not asked yet)
     int opt[SPOTLIGHT_OPT_COUNT];    // spotlight_set_option
     const void* big_lds_kernels[16]; // kernels whose dynamic LDS limit has been raised already
@@ -188,6 +192,16 @@ int launch_retrieve(spotlight_ctx* ctx, const uint32_t* codes, int64_t n_tokens,
 int launch_attend(spotlight_ctx* ctx, const void* q, const void* K, const void* V,
                   const int32_t* idx, int k, float scale, float* out);
 
+// The 8-bit cache (cache.h).  `first` and `count` may be null.
+int launch_cache_write(spotlight_ctx* ctx, const spotlight_cache& c, const void* K, const void* V, int64_t t0, int64_t n,
+                       const int32_t* first, const int32_t* count);
+int launch_cache_read(spotlight_ctx* ctx, const spotlight_cache& c, int64_t t0, int64_t n, const int32_t* first, void* K, void* V);
+int launch_cache_attend(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, const int32_t* idx, int k, float scale, float* out);
+int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, int64_t n_tokens, int n_q, const int32_t* lens,
+                       float scale, float* out);
+// Joins the nsplit partial results {max in units of log2, sum} and sums of values of each row.
+int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const float* part_acc, int64_t rows, int nsplit, float* out);
+
 // Error bound of the matrix-core last hash layer per unit of ||W2[j]|| * ||h||, n terms long (hash_bulk.h): the rounding of
 // partial sums, which are at most as large as the terms before them or as the result and the terms behind them,
 // by the binary32 chain (n / 2) and between the groups of eight that the matrix core adds (three times n / 8 groups, of hi and
@@ -203,6 +217,12 @@ bool step_small_applies(const spotlight_ctx* ctx, int64_t n_tokens);
 int launch_step_small(spotlight_ctx* ctx, const HashLaunch& qjob, const HashLaunch& kjob, const void* q, const void* K,
                       const void* V, const uint32_t* codes, int64_t n_tokens, int k, int n_sink, int n_local,
                       float scale, int32_t* out_idx, float* out);
+
+// Hash jobs of the entry points: n_new key rows of every (batch, kv head), rows t0 .. of K [B, Hkv, Nmax, d], and the queries.
+HashLaunch key_job(const spotlight_ctx* ctx, const void* K, const spotlight_hash_weights* w, int64_t t0, int64_t n_new, uint32_t* codes);
+HashLaunch query_job(const spotlight_ctx* ctx, const void* q, const spotlight_hash_weights* w);
+bool misaligned(const void* p);
+int check_weights(const spotlight_ctx* ctx, const spotlight_hash_weights* w);
 
 // Host-only argument checks of the decode step (SPOTLIGHT_OK or the error spotlight_decode_step returns).
 int check_step_args(const spotlight_ctx* ctx, const void* q, const void* K, const void* V, const spotlight_hash_weights* w,

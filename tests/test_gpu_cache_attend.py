@@ -1,0 +1,284 @@
+"""Attention over the 8-bit cache: over gathered rows and over the whole cache, against 64-bit attention on the values that
+the codes stand for."""
+import math
+
+import pytest
+import torch
+
+import cache_common as cc
+import paper_2508_19740_amd as sp
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SCALE = 1.0 / math.sqrt(128)
+
+
+def _ctx(b, hq, hkv, n, k=1, kv="bf16"):
+    return sp.Spotlight(b, hq, hkv, 128, 256, n, k, kv_dtype=cc.KV[kv], device=DEV)
+
+
+def _q(seed, kv, *shape, size=1.0):
+    return (torch.randn(*shape, cc.D, generator=torch.Generator().manual_seed(seed)) * size).to(cc.KV[kv])
+
+
+def _check(got, want, tol, what):
+    got = got.cpu().double()
+    bad = ~((got - want).abs() <= tol)
+    bad &= ~(torch.isnan(want) & torch.isnan(got))
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} off, worst {float((got - want).abs().nan_to_num(9e9).max())}, allowed there {float(tol[bad].min())}"
+
+
+# ------------------------------------------------------------------------------------------ gathered rows
+
+SPARSE = [  # b, hq, hkv, n, k, block, code, kv
+    (1, 1, 1, 1, 1, 16, "e4m3", "bf16"),
+    (1, 1, 1, 40, 7, 16, "i8", "f32"),
+    (2, 6, 3, 700, 20, 32, "e4m3", "f32"),
+    (1, 8, 1, 900, 128, 64, "i8", "bf16"),
+    (1, 7, 1, 900, 129, 128, "e4m3", "bf16"),
+    (3, 4, 2, 900, 256, 64, "i8", "f32"),
+    (2, 4, 4, 1500, 257, 16, "e4m3", "bf16"),
+    (1, 2, 1, 5000, 1111, 32, "i8", "bf16"),
+    (2, 32, 8, 5000, 2048, 64, "e4m3", "bf16"),
+    (1, 16, 16, 5000, 4999, 128, "i8", "f32"),
+]
+
+
+@pytest.mark.parametrize("b,hq,hkv,n,k,block,code,kv", SPARSE)
+def test_gathered_rows(b, hq, hkv, n, k, block, code, kv):
+    host = cc.random_cache(b, hkv, n, block, code, 11)
+    ctx, cache = _ctx(b, hq, hkv, n, k, kv), host.device()
+    g = torch.Generator().manual_seed(7)
+    q = _q(3, kv, b, hq, size=2.0)
+    idx = torch.randint(0, n, (b, hq, k), generator=g, dtype=torch.int32)        # any order, some twice
+    idx[torch.rand(b, hq, k, generator=g) < 0.05] = -1                           # and some outside the cache
+    idx[torch.rand(b, hq, k, generator=g) < 0.02] = n + 3
+    if k > 1:
+        idx[0, 0] = n                                                            # a head with no row at all
+    out = ctx.sparse_decode_cache(q.to(DEV), cache, idx.to(DEV), SCALE)
+    for i in range(b):
+        for h in range(hq):
+            t = idx[i, h].long()
+            t = t[(t >= 0) & (t < n)]
+            kk, vv = (host.values(x)[i, h // (hq // hkv), t] for x in "kv")
+            want, mag, size = cc.attention(q[i, h][None], kk, vv, torch.ones(1, t.numel(), dtype=torch.bool), SCALE) if t.numel() else \
+                (torch.zeros(1, cc.D, dtype=torch.float64),) * 2 + (torch.zeros(1, 1, dtype=torch.float64),)
+            _check(out[i, h][None], want, cc.tolerance(mag, size, 64), f"batch {i} head {h}")
+    assert k == 1 or float(out[0, 0].abs().max()) == 0.0
+    ctx.close()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+def test_gathered_rows_with_nan(code):
+    """A NaN is seen by the heads that list its row (integers: a row of its block), and by no other; row 0, which stands in for
+    rows that are missing, is one."""
+    b, hq, hkv, n, k, block = 1, 4, 1, 400, 300, 16
+    host = cc.random_cache(b, hkv, n, block, code, 2)
+    for x in "kv":
+        if code == "e4m3":
+            host.codes[x][0, 0, 0, 3] = math.nan
+        else:
+            host.scale[x][0, 0, 0] = math.nan
+    for kk in (20, k):
+        ctx, cache = _ctx(b, hq, hkv, n, kk), host.device()
+        q = _q(3, "bf16", b, hq)
+        idx = torch.randint(16, n, (b, hq, kk), dtype=torch.int32, generator=torch.Generator().manual_seed(1))
+        idx[0, 1, 5:] = -1
+        idx[0, 2, kk // 2] = 0
+        idx[0, 3] = -1
+        out = ctx.sparse_decode_cache(q.to(DEV), cache, idx.to(DEV), SCALE).cpu()
+        assert bool(torch.isfinite(out[0, :2]).all())
+        assert bool(torch.isnan(out[0, 2]).all())                              # the key's score is NaN
+        assert float(out[0, 3].abs().max()) == 0.0
+        ctx.close()
+
+
+# ------------------------------------------------------------------------------------------ the whole cache
+
+DENSE = [  # b, hq, hkv, n, n_q, block, code, kv, lens
+    (1, 1, 1, 1, 1, 16, "e4m3", "bf16", None),
+    (1, 1, 1, 1, 1, 16, "i8", "f32", None),
+    (1, 1, 1, 31, 1, 16, "e4m3", "f32", None),
+    (2, 8, 1, 33, 2, 32, "i8", "bf16", [33, 1]),
+    (1, 7, 1, 127, 1, 64, "e4m3", "bf16", None),
+    (3, 4, 2, 129, 1, 128, "i8", "bf16", [129, 0, 64]),
+    (2, 6, 3, 500, 5, 16, "e4m3", "f32", [500, 3]),                            # the second sequence: two queries before its start
+    (1, 8, 8, 1000, 16, 32, "i8", "f32", None),
+    (2, 4, 4, 1000, 17, 64, "e4m3", "bf16", [17, 993]),
+    (1, 4, 1, 1500, 33, 16, "i8", "bf16", None),
+    (1, 8, 2, 1500, 40, 128, "e4m3", "f32", [777]),
+    (1, 16, 2, 700, 700, 64, "e4m3", "bf16", None),                            # a whole prompt
+    (2, 8, 1, 2500, 1, 64, "i8", "bf16", [-4, 9000]),                          # lengths out of range: taken into it
+    (16, 8, 2, 300, 3, 32, "e4m3", "bf16", list(range(0, 320, 20))),
+    (1, 2, 1, 20011, 1, 64, "e4m3", "bf16", None),
+]
+
+
+def _dense(host, q, n, lens, i, h, group, nq):
+    ln = min(max(lens[i], 0), n) if lens is not None else n
+    t = torch.arange(n)
+    seen = t[None] <= (ln - nq + torch.arange(nq))[:, None]
+    k, v = (host.values(x)[i, h // group, :n] for x in "kv")
+    return cc.attention(q[i, h], k, v, seen, SCALE)
+
+
+@pytest.mark.parametrize("b,hq,hkv,n,nq,block,code,kv,lens", DENSE)
+def test_the_whole_cache(b, hq, hkv, n, nq, block, code, kv, lens):
+    cap = n + 5
+    host = cc.random_cache(b, hkv, cap, block, code, 4)
+    # rows behind a sequence hold anything: they are not read
+    for i in range(b):
+        ln = min(max(lens[i], 0), n) if lens is not None else n
+        if code == "e4m3":
+            for x in "kv":
+                host.codes[x][i, :, ln:] = math.nan
+        else:
+            for x in "kv":
+                host.scale[x][i, :, -(-ln // block):] = math.nan
+    ctx, cache = _ctx(b, hq, hkv, cap, 1, kv), host.device()
+    q = _q(5, kv, b, hq, nq, size=2.0)
+    ld = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+    out = ctx.dense_decode_cache(q.to(DEV), cache, n, ld, SCALE)
+    for i in range(b):
+        for h in range(hq):
+            want, mag, size = _dense(host, q, n, lens, i, h, hq // hkv, nq)
+            _check(out[i, h], want, cc.tolerance(mag, size, 32 + n // 8, 2 if kv == "f32" else 1, 2.0 ** -20) + cc.split_floor(host.values("v")[i, h // (hq // hkv), :n]),
+                   f"batch {i} head {h}")
+    if nq == 1:
+        assert torch.equal(out[:, :, 0], ctx.dense_decode_cache(q[:, :, 0].contiguous().to(DEV), cache, n, ld, SCALE))
+    ctx.close()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("nq", [3, 20, 70])
+def test_nan_reaches_only_the_queries_that_see_it(code, nq):
+    """NaN in K and V of tokens between the queries: those before it get the result without it."""
+    b, hq, hkv, n, block = 1, 4, 2, 400, 16
+    host = cc.random_cache(b, hkv, n, block, code, 6)
+    at = n - nq // 2 - 1 if code == "e4m3" else (n - 1) // block * block       # the token, or the block's first
+    ctx = _ctx(b, hq, hkv, n)
+    q = _q(8, "bf16", b, hq, nq)
+    for which in ("k", "v", "kv"):
+        h2 = cc.HostCache(b, hkv, n, block, code)
+        h2.codes = {x: host.codes[x].clone() for x in "kv"}
+        h2.scale = {x: host.scale[x].clone() for x in "kv"}
+        for x in which:
+            if code == "e4m3":
+                h2.codes[x][0, 0, at, 5] = math.nan
+            else:
+                h2.scale[x][0, 0, at // block] = math.nan
+        out = ctx.dense_decode_cache(q.to(DEV), h2.device(), n, None, SCALE).cpu()
+        for h in range(hq):
+            for i in range(nq):
+                last = n - nq + i
+                hit = h // 2 == 0 and last >= at
+                if hit:
+                    nan = torch.isnan(out[0, h, i])
+                    assert bool(nan[5]) and (bool(nan.all()) or (code == "e4m3" and which == "v" and int(nan.sum()) == 1)), (which, h, i)
+                else:
+                    v = torch.where(torch.isnan(h2.values("v")), 0.0, h2.values("v"))[0, h // 2, :last + 1]
+                    k = torch.where(torch.isnan(h2.values("k")), 0.0, h2.values("k"))[0, h // 2, :last + 1]
+                    want, mag, size = cc.attention(q[0, h, i][None], k, v, torch.ones(1, last + 1, dtype=torch.bool), SCALE)
+                    _check(out[0, h, i][None], want, cc.tolerance(mag, size, 32 + n // 8, 1, 2.0 ** -20) + cc.split_floor(v), (which, h, i))
+    ctx.close()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+def test_sizes_far_apart(code, kv):
+    """Blocks whose scales differ by up to 2^20, queries of very small and very large size, and a scale of either sign."""
+    b, hq, hkv, n, block = 1, 2, 1, 640, 16
+    host = cc.random_cache(b, hkv, n, block, code, 9)
+    g = torch.Generator().manual_seed(2)
+    host.scale["v"] *= torch.exp2(-torch.randint(0, 20, host.scale["v"].shape, generator=g).double())
+    host.scale["k"] *= torch.exp2(-torch.randint(0, 6, host.scale["k"].shape, generator=g).double())
+    ctx, cache = _ctx(b, hq, hkv, n, 64, kv), host.device()
+    for size, scale in ((1e-30, SCALE * 1e30), (1e30, SCALE * 1e-30), (1.0, -SCALE), (1.0, 0.0)):
+        q = _q(4, kv, b, hq, 2, size=size)
+        out = ctx.dense_decode_cache(q.to(DEV), cache, n, None, scale)
+        idx = torch.arange(0, n, 10, dtype=torch.int32).view(1, 1, -1).repeat(1, hq, 1)
+        sparse = ctx.sparse_decode_cache(q[:, :, 0].contiguous().to(DEV), cache, idx.to(DEV), scale)
+        t = torch.arange(n)
+        k, v = (host.values(x)[0, 0] for x in "kv")
+        for h in range(hq):
+            seen = t[None] <= (n - 2 + torch.arange(2))[:, None]
+            want, mag, sz = cc.attention(q[0, h], k, v, seen, scale)
+            # values below the run's largest by more than 2^20 lose up to 2^-30 of that
+            _check(out[0, h], want, cc.tolerance(mag, sz, 32 + n // 8, 2 if kv == "f32" else 1, 2.0 ** -20) + 2.0 ** -30 * float(v.abs().max()) + cc.split_floor(v), (size, scale, h))
+            want, mag, sz = cc.attention(q[0, h, :1], k[idx[0, 0].long()], v[idx[0, 0].long()], torch.ones(1, 64, dtype=torch.bool), scale)
+            _check(sparse[0, h][None], want, cc.tolerance(mag, sz, 64), (size, scale, h))
+    ctx.close()
+
+
+def test_one_key_takes_all():
+    """A key that is all the weight, among keys whose weights underflow together but not one by one."""
+    b, n, block = 1, 4096, 64
+    host = cc.HostCache(b, 1, n, block, "i8")
+    host.codes["k"][0, 0, :, 0] = -100.0
+    host.codes["k"][0, 0, 1234, 0] = 100.0
+    host.codes["v"][0, 0] = torch.randint(-127, 128, (n, cc.D), generator=torch.Generator().manual_seed(1)).double()
+    host.codes["v"][0, 0, 1234] = 1.0
+    ctx, cache = _ctx(b, 1, 1, n), host.device()
+    for gap in (5.0, 15.0, 25.0):                       # nats between the key and the others
+        q = torch.zeros(1, 1, 1, cc.D, dtype=torch.bfloat16)
+        q[..., 0] = 1.0
+        scale = gap / 200.0
+        out = ctx.dense_decode_cache(q.to(DEV), cache, n, None, scale)
+        want, mag, size = cc.attention(q[0, 0], host.values("k")[0, 0], host.values("v")[0, 0], torch.ones(1, n, dtype=torch.bool), scale)
+        _check(out[0, 0], want, cc.tolerance(mag, size, 32 + n // 8, 1, 2.0 ** -20) + cc.split_floor(host.values("v")[0, 0]), gap)
+    ctx.close()
+
+
+def test_refusals():
+    ctx = _ctx(2, 4, 2, 100, 10)
+    cache = ctx.new_cache(torch.int8, 32)
+    q = torch.zeros(2, 4, 128, dtype=torch.bfloat16, device=DEV)
+    for bad in (q.float(), q[:, :2].contiguous(), q.cpu(), q.view(2, 4, 128, 1).transpose(2, 3)[..., ::2]):
+        with pytest.raises(ValueError):
+            ctx.dense_decode_cache(bad, cache, 100)
+    for bad in (torch.zeros(2, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            ctx.dense_decode_cache(q, cache, 100, bad)
+    for n in (0, 101, -1):
+        with pytest.raises(sp.SpotlightError) as e:
+            ctx.dense_decode_cache(q, cache, n)
+        assert e.value.rc == sp.ERR_INVALID_ARG
+    idx = torch.zeros(2, 4, 11, dtype=torch.int32, device=DEV)
+    with pytest.raises(sp.SpotlightError):
+        ctx.sparse_decode_cache(q, cache, idx)
+    with pytest.raises(ValueError):
+        ctx.sparse_decode_cache(q, cache, idx[..., :5].long())
+    with pytest.raises(ValueError):
+        ctx.sparse_decode_cache(q, cache, idx[0])
+    ctx.close()
+
+
+def test_a_graph_and_stages():
+    """A captured call replayed over a cache that grows (lengths in device memory), eager work between the replays; and the
+    stages that a call is counted under."""
+    b, hq, hkv, n, block = 2, 8, 2, 3000, 64
+    host = cc.random_cache(b, hkv, n, block, "e4m3", 13)
+    ctx, cache = _ctx(b, hq, hkv, n), host.device()
+    q = _q(1, "bf16", b, hq, 2).to(DEV)
+    lens = torch.tensor([n, n], dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ctx.dense_decode_cache(q, cache, n, lens)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ctx.dense_decode_cache(q, cache, n, lens)
+    for a in ([1, 2], [500, 1777], [n, 64], [0, n]):
+        lens.copy_(torch.tensor(a, dtype=torch.int32))
+        graph.replay()
+        got = out.clone()
+        eager = ctx.dense_decode_cache(q, cache, n, lens)
+        assert torch.equal(got, eager)
+        torch.cuda.synchronize()
+    ctx.profile_enable(True)
+    ctx.dense_decode_cache(q, cache, n)
+    prof = ctx.profile_read()
+    ctx.profile_enable(False)
+    assert prof["attend"][1] == 1 and prof["merge"][1] == 1
+    ctx.close()
