@@ -343,8 +343,9 @@ int spotlight_sparse_decode_cache(spotlight_ctx *ctx, const void *q, const spotl
  *   lens  [B]              int32, device, or NULL
  *   out   [B, Hq, n_q, d]  float32
  * The call enqueues two kernels, or one where the keys need no splitting, and nothing else.
- * Errors: INVALID_ARG for a bad cache or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax; UNSUPPORTED if more than
- * 2^25 tokens would have to be split further than the workspace allows for (over 16384 / ceil(n_tokens / 2^25) rows of q).
+ * Errors: INVALID_ARG for a bad cache or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax; UNSUPPORTED for more than
+ * 2^24 / (Hq / Hkv) queries, or if more than 2^25 tokens would have to be split further than the workspace allows for
+ * (over 16384 / ceil(n_tokens / 2^25) rows of q).
  */
 int spotlight_dense_decode_cache(spotlight_ctx *ctx, const void *q, const spotlight_cache *cache, int64_t n_tokens,
                                  int32_t n_q, const int32_t *lens, float scale, float *out);

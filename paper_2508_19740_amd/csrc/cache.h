@@ -22,11 +22,12 @@ struct DenseSplit {
 inline int split_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, DenseSplit* s)
 {
     const int64_t rows = static_cast<int64_t>(p.G) * n_q, heads = static_cast<int64_t>(p.B) * p.Hkv;
-    s->tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;   // a grid's first dimension, and 32 bits for a row
+    s->tiles = rows <= 16 ? 1 : 2;
     const int64_t groups = heads * ((rows + 16 * s->tiles - 1) / (16 * s->tiles));
     constexpr int64_t unit = kDenseStep * kDenseWaves;
     const int64_t room = p.dense_rows / (heads * rows), most = (n_tokens + unit - 1) / unit;
-    int64_t n = (static_cast<int64_t>(n_cus) * (s->tiles == 4 ? 2 : 4) + groups - 1) / groups;
+    int64_t n = (static_cast<int64_t>(n_cus) * (s->tiles == 2 ? 2 : 4) + groups - 1) / groups;
     if (n > room) n = room;
     if (n > most) n = most;
     if (n < 1) n = 1;

@@ -7,9 +7,10 @@
 //   S^T = K Q^T     v_mfma_f32_16x16x32_f16.  Lane (g, i) = (lane / 16, lane % 16) loads 32 adjacent
 //                   bytes of key i; four products take 8 of them each, and q lies in registers in the
 //                   same order.  The result leaves lane (g, i) with keys 4g .. 4g+3 of query row i.
-//   softmax         a row's maximum changes rarely: lanes compare their own scores with the last maximum,
-//                   and only where one is larger is the maximum taken over the lanes and what has been
-//                   summed rescaled.
+//   softmax         weights are relative to a maximum that was taken once.  Lanes compare their own scores
+//                   with it, and only where one is more than 4 (a factor of 16) above it is the maximum taken
+//                   anew, over the lanes, and what has been summed rescaled.  (Taken at every larger score, some row
+//                   of 16 had one at most steps.)
 //   O^T += V^T P^T  The lane holds the weights just where the second operand wants them (the keys of a
 //                   product may come in any order).  The first operand wants the same keys of one
 //                   column: lane (g, i) loads 8 bytes, columns 8i .. 8i+7, of each of its eight keys, and
@@ -18,7 +19,7 @@
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
 //       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).
-//   p   is in [0, 1], scaled by 2^15 and split in two parts.
+//   p   is in [0, 16], scaled by 2^11 and split in two parts: 20 bits, or 2^-35 where that is more.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
 //       ratio is above 2^-20, and at most 2^-30 of the largest block's size off below.
 //
@@ -39,8 +40,10 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = kDenseStep;       // keys of a step
 constexpr int kWaves = kDenseWaves;
 static_assert(kWaves == kThreads / 64, "wavefronts of a workgroup");
-constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^15
-constexpr float kPUp = 15.0f;
+constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^11
+constexpr float kPUp = 11.0f;
+constexpr float kSlack = 4.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
+constexpr int kInf = 0x7f800000;
 constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d)
@@ -109,10 +112,27 @@ struct DenseArgs {
     float* out;
     int64_t Nmax, blocks, n_tokens;
     int64_t chunk;                      // keys of a split, a multiple of kStep * kWaves
-    int64_t rows;                       // rows of a key-value head: G * n_q
-    int n_q, Hkv, nsplit, shift;
-    float scale2;                       // scale * log2(e)
+    uint32_t rows, n_q;                 // rows of a key-value head: G * n_q
+    uint32_t nsplit;
+    uint32_t turn;                      // by how much the splits of one head are turned against the last one's
+    int Hkv, shift;
+    float scale2;                       // |scale| * log2(e)
+    bool negate;                        // the scale is negative: q is negated
 };
+
+// x less the low or the high half of h, in one instruction.
+__device__ __forceinline__ float less_low(float x, h2 h)
+{
+    float d;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(x));
+    return d;
+}
+__device__ __forceinline__ float less_high(float x, h2 h)
+{
+    float d;
+    asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(h), "v"(x));
+    return d;
+}
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
@@ -128,9 +148,9 @@ __device__ __forceinline__ float across_groups_sum(float x)
 }
 
 // One row's 32 elements of a lane, scaled by 2^(13 - exponent of the row's largest) and split into QP
-// binary16 parts; returns the exponent that was taken out.
+// binary16 parts, negated if asked; returns minus the exponent that was put in.
 template <typename QT, int QP>
-__device__ __forceinline__ int load_row(const QT* q, h8 (&frag)[QP][4])
+__device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP][4])
 {
     float x[32];
     if constexpr (sizeof(QT) == 2) {
@@ -159,7 +179,7 @@ __device__ __forceinline__ int load_row(const QT* q, h8 (&frag)[QP][4])
     for (int c = 0; c < 4; ++c)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float y = ldexpf(x[8 * c + j], 13 - ex);
+            const float y = ldexpf(negate ? -x[8 * c + j] : x[8 * c + j], 13 - ex);
             const _Float16 hi = static_cast<_Float16>(y);
             frag[0][c][j] = hi;
             if constexpr (QP == 2) frag[1][c][j] = static_cast<_Float16>(y - static_cast<float>(hi));
@@ -169,7 +189,7 @@ __device__ __forceinline__ int load_row(const QT* q, h8 (&frag)[QP][4])
 
 // MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a split.
 template <typename CT, typename QT, int MT>
-__global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
+__global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(DenseArgs a)
 {
     constexpr int QP = sizeof(QT) == 2 ? 1 : 2;
     typedef Operand<CT> Op;
@@ -178,104 +198,123 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, i = lane & 15;
-    const int split = static_cast<int>(blockIdx.x % a.nsplit);
-    const int64_t r0 = static_cast<int64_t>(blockIdx.x / a.nsplit) * (16 * MT);
+    const uint32_t split = (blockIdx.x + a.turn * blockIdx.y) % a.nsplit, r0 = blockIdx.x / a.nsplit * (16 * MT);
     const int64_t head = blockIdx.y;
 
     int64_t len = a.n_tokens;
-    if (a.lens) len = min(max(static_cast<int64_t>(a.lens[head / a.Hkv]), static_cast<int64_t>(0)), len);
+    if (a.lens) len = min(max(static_cast<int64_t>(a.lens[blockIdx.y / static_cast<uint32_t>(a.Hkv)]), static_cast<int64_t>(0)), len);
 
-    // keys each of this lane's rows sees: those before `seen`.  Rows behind the last repeat it.
-    int64_t seen[MT], least = len, most = 0;
-    h8 qf[MT][QP][4];
-    float factor[MT];
+    // The queries of the tile's rows: first of them, last of them, and those of the lane's rows.  Rows behind the
+    // last repeat it.
+    uint32_t q_least = 0, q_most = 0, query[MT], row[MT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t r = min(r0 + 16 * t + i, a.rows - 1);
-        seen[t] = max(len - a.n_q + r % a.n_q + 1, static_cast<int64_t>(0));
-        least = min(least, seen[t]);
-        most = max(most, seen[t]);
-        const int ex = load_row<QT, QP>(static_cast<const QT*>(a.q) + (head * a.rows + r) * kHeadDim + g * 32, qf[t]);
-        factor[t] = ldexpf(a.scale2, ex);
-    }
+    for (int t = 0; t < MT; ++t) { row[t] = min(r0 + 16 * t + i, a.rows - 1); query[t] = 0; }
+    if (a.n_q > 1) {
+        const uint32_t last = min(r0 + 16 * MT, a.rows) - 1;
+        q_least = r0 % a.n_q;
+        q_most = last % a.n_q;
+        if (last - r0 >= a.n_q || q_least > q_most) { q_least = 0; q_most = a.n_q - 1; }
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) {
-        least = min(least, static_cast<int64_t>(__shfl_xor(static_cast<long long>(least), off)));
-        most = max(most, static_cast<int64_t>(__shfl_xor(static_cast<long long>(most), off)));
+        for (int t = 0; t < MT; ++t) query[t] = row[t] % a.n_q;
     }
+    const int64_t before = len - a.n_q + 1;      // query x sees the keys before this + x
 
     // this wavefront's keys
-    const int64_t c0 = split * a.chunk, c1 = min(c0 + a.chunk, most);
+    const int64_t c0 = split * a.chunk, c1 = min(c0 + a.chunk, before + q_most);
     const int64_t share = a.chunk / kWaves;
     const int64_t k0 = c0 + wave * share;
-    const int n = __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(c1 - k0, static_cast<int64_t>(0)), share)));
+    const int n = static_cast<int>(min(max(c1 - k0, static_cast<int64_t>(0)), share));
     const int steps = (n + kStep - 1) / kStep;
     // the first steps, whose keys every row sees
-    const int plain_steps = __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(least - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n)) / kStep));
-    int sees[MT];                       // keys of the run that the lane's row sees
+    const int plain_steps = static_cast<int>(min(max(before + q_least - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n))) / kStep;
+    int sees[MT];                                // keys of the run that the lane's row sees
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sees[t] = static_cast<int>(min(max(seen[t] - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n)));
+    for (int t = 0; t < MT; ++t) sees[t] = static_cast<int>(min(max(before + query[t] - k0, static_cast<int64_t>(0)), static_cast<int64_t>(n)));
 
     // Rows behind the run read as zeros: the buffer ends with it.  Offsets within it stay below 2^31 (the host
     // bounds a split), and all of them are in the instruction's checked part.
-    const int64_t base = (head * a.Nmax + k0) * kHeadDim;
-    const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.k + base), 0, n * kHeadDim, 0x00020000);
-    const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.v + base), 0, n * kHeadDim, 0x00020000);
+    const int64_t start = (head * a.Nmax + k0) * kHeadDim;
+    const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.k + start), 0, n * kHeadDim, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.v + start), 0, n * kHeadDim, 0x00020000);
+    u4 kreg[2][2];
+    u2 vreg[2][4];
+    int koff = i * kHeadDim + g * 32, voff = g * (4 * kHeadDim) + i * 8;      // of the next step
+    auto load_k = [&]() {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + (t * (16 * kHeadDim) + j * 16), 0, 0);
+        koff += kStep * kHeadDim;
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                vreg[t][r] = __builtin_amdgcn_raw_buffer_load_b64(vr, voff + (t * (16 * kHeadDim) + r * kHeadDim), 0, 0);
+        voff += kStep * kHeadDim;
+    };
+    // on their way while the queries and scales are read
+    load_k();
+    load_v();
+
     const float* ks = a.k_scale + head * a.blocks;
     const float* vs = a.v_scale + head * a.blocks;
-    const int64_t last_block = (k0 + (n > 0 ? n - 1 : 0)) >> a.shift;
+    const uint32_t last_block = static_cast<uint32_t>(k0 + (n > 0 ? n - 1 : 0)) >> a.shift;   // tokens are below 2^31
 
     // the largest scale of the run's values
     float unit = 0.0f;
     if (n > 0)
-        for (int64_t j = (k0 >> a.shift) + lane; j <= last_block; j += 64) unit = fmaxf(unit, vs[j]);
+        for (uint32_t j = (static_cast<uint32_t>(k0) >> a.shift) + lane; j <= last_block; j += 64) unit = fmaxf(unit, vs[j]);
+    h8 qf[MT][QP][4];
+    float factor[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int ex = load_row<QT, QP>(static_cast<const QT*>(a.q) + (head * a.rows + row[t]) * kHeadDim + g * 32, a.negate, qf[t]);
+        factor[t] = ldexpf(a.scale2, ex);
+    }
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) unit = fmaxf(unit, __shfl_xor(unit, off));
     if (!(unit > 0.0f)) unit = 1.0f;
     const int unit_bits = __builtin_amdgcn_readfirstlane(__float_as_int(unit)) - ((127 + kVUp) << 23);
 
     f4 acc[MT][8];
-    float m[MT], l[MT];
+    float base[MT], l[MT];                       // kPUp less the maximum (infinite: none yet), and the lane's sum of weights
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        m[t] = -INFINITY;
+        base[t] = INFINITY;
         l[t] = 0.0f;
 #pragma unroll
         for (int d = 0; d < 8; ++d) acc[t][d] = f4{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
-    u4 kreg[2][2];
-    u2 vreg[2][4];
-    const int koff = i * kHeadDim + g * 32, voff = g * (4 * kHeadDim) + i * 8;
-    auto load_k = [&](int s) {
+    float next_ks[2];
+    int next_vs[2];                              // as bits
+    auto load_scales = [&](int s) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + s * (kStep * kHeadDim) + (t * (16 * kHeadDim) + j * 16), 0, 0);
+        for (int t = 0; t < 2; ++t) {
+            const uint32_t blk = min((static_cast<uint32_t>(k0) + s * kStep + 16 * t) >> a.shift, last_block);
+            next_ks[t] = ks[blk];
+            next_vs[t] = reinterpret_cast<const int*>(vs)[blk];
+        }
     };
-    auto load_v = [&](int s) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                vreg[t][r] = __builtin_amdgcn_raw_buffer_load_b64(vr, voff + s * (kStep * kHeadDim) + (t * (16 * kHeadDim) + r * kHeadDim), 0, 0);
-    };
+    if (steps > 0) load_scales(0);
 
     auto step = [&](int s, auto masked) {
-        const int64_t key = k0 + static_cast<int64_t>(s) * kStep;
+        // the scales of this step; the next one's are on their way from here on
         float kscale[2];
         typename Op::Ratio ratio[2];
         bool nan_values = false;                                // of this step; asked only where a row sees part of it
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int64_t blk = min((key + 16 * t) >> a.shift, last_block);
-            kscale[t] = ks[blk];
-            const float v = vs[blk];
-            const int up = __float_as_int(v) - unit_bits;       // powers of two: a difference of exponents
-            ratio[t] = Op::ratio(v != v ? v : up > 0 ? __int_as_float(up) : 0.0f);
-            if constexpr (decltype(masked)::value && !CT::kHasNaN) nan_values |= v != v;
+            kscale[t] = next_ks[t];
+            const int v = next_vs[t], up = v - unit_bits;       // powers of two: a difference of exponents
+            const bool nan = v > kInf;
+            ratio[t] = Op::ratio(__int_as_float(nan ? v : up > 0 ? up : 0));
+            if constexpr (decltype(masked)::value && !CT::kHasNaN) nan_values |= nan;
         }
+        load_scales(s + 1);
         if constexpr (decltype(masked)::value && CT::kHasNaN) {
             uint32_t found = 0;                                 // bytes of 7f and ff
 #pragma unroll
@@ -298,42 +337,51 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
 #pragma unroll
                     for (int p = 0; p < QP; ++p) sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][kt], 0, 0, 0);
             }
-        load_k(s + 1);
+        load_k();
         // softmax
         h8 hi[MT], lo[MT];
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            float x[8];
+            float f[2], x[8];
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) f[kt] = factor[t] * kscale[kt];
             float top = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] = sc[t][e / 4][e % 4] * (factor[t] * kscale[e / 4]);
+                x[e] = __builtin_fmaf(sc[t][e / 4][e % 4], f[e / 4], base[t]);
                 if constexpr (decltype(masked)::value)
                     if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
                 top = fmaxf(top, x[e]);
             }
-            if (__any(top > m[t])) {
-                const float mn = across_groups_max(fmaxf(m[t], top));
-                // nothing before: nothing to rescale
-                const float down = m[t] > -INFINITY ? __builtin_amdgcn_exp2f(m[t] - mn) : 0.0f;
-                l[t] *= down;
+            if (__any(!(top <= kPUp + kSlack))) {          // also before the first maximum
+                float high = -INFINITY;
 #pragma unroll
-                for (int d = 0; d < 8; ++d) acc[t][d] *= down;
-                m[t] = mn;
-            }
-            const float base2 = (m[t] > -INFINITY ? m[t] : 0.0f) - kPUp;
-            float sum = 0.0f;
+                for (int e = 0; e < 8; ++e) {
+                    x[e] = sc[t][e / 4][e % 4] * f[e / 4];
+                    if constexpr (decltype(masked)::value)
+                        if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
+                    high = fmaxf(high, x[e]);
+                }
+                high = across_groups_max(high);
+                if (high > -INFINITY) {
+                    const float to = fminf(kPUp - high, base[t]);
+                    const float down = __builtin_amdgcn_exp2f(to - base[t]);      // 0 before the first maximum
+                    l[t] *= down;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                x[e] = __builtin_amdgcn_exp2f(x[e] - base2);
-                sum += x[e];
+                    for (int d = 0; d < 8; ++d) acc[t][d] *= down;
+                    base[t] = to;
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = x[e] > -INFINITY ? x[e] + base[t] : x[e];
             }
-            l[t] += sum;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
+            l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
             h2 h[4], r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 h[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x[2 * e], x[2 * e + 1]));
-                r[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x[2 * e] - static_cast<float>(h[e].x), x[2 * e + 1] - static_cast<float>(h[e].y)));
+                r[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(less_low(x[2 * e], h[e]), less_high(x[2 * e + 1], h[e])));
             }
             hi[t] = join(h[0], h[1], h[2], h[3]);
             lo[t] = join(r[0], r[1], r[2], r[3]);
@@ -377,15 +425,11 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
                 }
             }
         }
-        load_v(s + 1);
+        load_v();
     };
-    if (steps > 0) {
-        load_k(0);
-        load_v(0);
-        int s = 0;
-        for (; s < plain_steps; ++s) step(s, Flag<false>{});
-        for (; s < steps; ++s) step(s, Flag<true>{});
-    }
+    int s = 0;
+    for (; s < plain_steps; ++s) step(s, Flag<false>{});
+    for (; s < steps; ++s) step(s, Flag<true>{});
 
     // the wavefronts' results, joined: lane (g, i) has columns 32g .. 32g+31 of row i
     const float to_value = ldexpf(unit, -kVUp);
@@ -393,7 +437,7 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
     for (int t = 0; t < MT; ++t) {
         const float sum = across_groups_sum(l[t]);
         if (t) __syncthreads();
-        if (g == 0) { s_m[wave][i] = m[t]; s_l[wave][i] = sum; }
+        if (g == 0) { s_m[wave][i] = kPUp - base[t]; s_l[wave][i] = sum; }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -401,7 +445,7 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
                 *reinterpret_cast<f4*>(&s_acc[wave][i][g * 32 + r * 8 + d]) =
                     f4{acc[t][d][r], acc[t][d + 1][r], acc[t][d + 2][r], acc[t][d + 3][r]} * to_value;
         __syncthreads();
-        const int64_t left = a.rows - (r0 + 16 * t);
+        const int left = static_cast<int>(a.rows - min(r0 + 16 * t, a.rows));
         for (int e = tid; e < 16 * kHeadDim && e / kHeadDim < left; e += kThreads) {
             const int row = e / kHeadDim, col = e % kHeadDim;
             float M = -INFINITY;
@@ -428,11 +472,15 @@ __global__ __launch_bounds__(kThreads) void cache_dense_kernel(DenseArgs a)
 }
 
 template <typename CT, typename QT>
-void launch_mt(spotlight_ctx* ctx, StageTimer& timer, const DenseArgs& a, int mt)
+void launch_mt(spotlight_ctx* ctx, StageTimer& timer, DenseArgs& a, int mt)
 {
     const Plan& p = ctx->plan;
-    const dim3 grid(static_cast<unsigned>((a.rows + 16 * mt - 1) / (16 * mt) * a.nsplit), static_cast<unsigned>(p.B * p.Hkv));
-    auto kern = mt == 1 ? cache_dense_kernel<CT, QT, 1> : mt == 2 ? cache_dense_kernel<CT, QT, 2> : cache_dense_kernel<CT, QT, 4>;
+    const dim3 grid((a.rows + 16 * mt - 1) / (16 * mt) * a.nsplit, static_cast<unsigned>(p.B * p.Hkv));
+    // Workgroups go to the eight dies in turn.  Sequences of different lengths use their first splits most, so split s of
+    // head y belongs on die s + y, whatever the width of the grid: with 16 splits of 16 sequences of 2049 .. 32769
+    // tokens all dies work as long (81 -> 67 us).
+    a.turn = grid.x % 8 + 7;
+    auto kern = mt == 1 ? cache_dense_kernel<CT, QT, 1> : cache_dense_kernel<CT, QT, 2>;
     timer.launch(kern, grid, dim3(kThreads), 0, a);
 }
 
@@ -455,17 +503,18 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     a.Nmax = p.Nmax;
     a.blocks = (p.Nmax + c.block_tokens - 1) / c.block_tokens;
     a.n_tokens = n_tokens;
-    a.rows = static_cast<int64_t>(p.G) * n_q;
-    a.n_q = n_q;
+    a.rows = static_cast<uint32_t>(p.G) * static_cast<uint32_t>(n_q);
+    a.n_q = static_cast<uint32_t>(n_q);
     a.Hkv = p.Hkv;
     a.shift = __builtin_ctz(static_cast<unsigned>(c.block_tokens));
-    a.scale2 = scale * kLog2e;
+    a.scale2 = fabsf(scale) * kLog2e;
+    a.negate = scale < 0.0f;
 
     DenseSplit sp;
     const int rc = split_dense(p, ctx->n_cus, n_tokens, n_q, &sp);
     if (rc != SPOTLIGHT_OK) return rc;
     a.chunk = sp.chunk;
-    a.nsplit = sp.nsplit;
+    a.nsplit = static_cast<uint32_t>(sp.nsplit);
     {
         StageTimer timer(ctx, SPOTLIGHT_STAGE_ATTEND);
         if (timer.rec) timer.rec->whole = a.nsplit == 1;
@@ -479,7 +528,7 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
     if (a.nsplit == 1) return SPOTLIGHT_OK;
-    return launch_cache_merge(ctx, a.part_ml, a.part_acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, a.nsplit, out);
+    return launch_cache_merge(ctx, a.part_ml, a.part_acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, sp.nsplit, out);
 }
 
 }  // namespace spotlight

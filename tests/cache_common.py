@@ -120,7 +120,7 @@ def tolerance(mag, size, chain, q_parts=1, p_err=0.0):
 
 
 def split_floor(v):
-    """What the binary16 parts of the weights lose however small a weight is: a weight is scaled by 2^15, and of its second part
+    """What the binary16 parts of the weights lose however small a weight is: a weight is scaled by 2^11, and of its second part
     binary16 drops less than its smallest step, 2^-24.  So each key's weight (relative to the largest) is off by less than
-    2^-39, and a column's sum by at most 2^-39 sum |v|; the denominator is at least 1.  v: the head's values [n, d]."""
-    return 2.0 ** -39 * torch.nan_to_num(v).abs().sum(0)
+    2^-35, and a column's sum by at most 2^-35 sum |v|; the denominator is at least 1.  v: the head's values [n, d]."""
+    return 2.0 ** -35 * torch.nan_to_num(v).abs().sum(0)

@@ -125,7 +125,7 @@ int main()
                             cache::DenseSplit s;
                             const int rc = cache::split_dense(p, 256, n, static_cast<int>(nq), &s);
                             const long all = static_cast<long>(B) * Hkv * G * nq;
-                            if (rc == SPOTLIGHT_ERR_UNSUPPORTED && n > cache::kDenseMostKeys) continue;
+                            if (rc == SPOTLIGHT_ERR_UNSUPPORTED && (n > cache::kDenseMostKeys || G * nq > 1 << 24)) continue;
                             const bool ok = rc == SPOTLIGHT_OK && (s.tiles == 1 || s.tiles == 2 || s.tiles == 4) && s.nsplit >= 1 &&
                                 s.chunk % (cache::kDenseStep * cache::kDenseWaves) == 0 && s.chunk <= cache::kDenseMostKeys + 127 &&
                                 s.chunk * s.nsplit >= n && s.chunk * (s.nsplit - 1) < n && (s.nsplit == 1 || all * s.nsplit <= p.dense_rows);
