@@ -73,6 +73,7 @@ int make_plan(const spotlight_config* c, Plan* p)
     p->dense_rows = most_rows < 16384 ? most_rows : 16384;
     p->off_dense_ml = off;  off = align_up(off + static_cast<size_t>(p->dense_rows) * 8, 256);
     p->off_dense_acc = off; off = align_up(off + static_cast<size_t>(p->dense_rows) * kHeadDim * 4, 256);
+    p->off_arrived = off;   off = align_up(off + kArrivedBytes, 256);
     p->off_audit = off;     off = align_up(off + sizeof(AuditRec), 256);
     p->total_bytes = off;
     return SPOTLIGHT_OK;
@@ -264,7 +265,9 @@ int spotlight_create(spotlight_ctx** out, const spotlight_config* cfg)
         return SPOTLIGHT_ERR_WORKSPACE;
     }
     ctx->workspace = static_cast<char*>(ws);
-    if (hipMemsetAsync(ctx->workspace + plan.off_audit, 0, sizeof(AuditRec), ctx->stream) != hipSuccess) {
+    if (hipMemsetAsync(ctx->workspace + plan.off_audit, 0, sizeof(AuditRec), ctx->stream) != hipSuccess ||
+        hipMemsetAsync(ctx->workspace + plan.off_arrived, 0, kArrivedBytes, ctx->stream) != hipSuccess ||
+        hipStreamSynchronize(ctx->stream) != hipSuccess) {
         (void)hipFree(ws);
         delete[] ctx->recs;
         delete ctx;

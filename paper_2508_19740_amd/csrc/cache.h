@@ -40,6 +40,17 @@ inline int split_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, Dens
     return SPOTLIGHT_OK;
 }
 
+// Whether the last workgroup of each group of rows joins its partial results, instead of a launch of its own: small
+// calls, where the join is one round of loads (about 2 us, since nothing of it is in a cache; a launch takes 3.5 us of the
+// host).  Against the merge kernel, called back to back: 1 head, 600 / 4096 / 8192 tokens 10.6 / 11.5 / 11.5 -> 8.7 / 8.4 /
+// 8.8 us, gathered 300 / 2000 of them 10.2 / 10.4 -> 7.8 / 7.7 us, and no slower in a graph; with two rounds, 16384
+// tokens 11.3 -> 11.2 us (graph 10.2 -> 11.2), 1000 tokens of 4 groups of 8, 11.6 -> 10.5 us (graph 9.0 -> 10.4).
+inline bool joins_in_place(int64_t groups, int64_t rows, int64_t nsplit)
+{
+    const int64_t rounds = rows >= 4 ? (rows + 3) / 4 * ((nsplit + 15) / 16) : rows * ((nsplit + 63) / 64);
+    return nsplit > 1 && rounds <= 1 && groups * nsplit <= kJoinGroups;
+}
+
 #if defined(__HIPCC__)
 
 struct bf16_raw { uint16_t v; };
@@ -93,6 +104,114 @@ __device__ __forceinline__ int least_exponent(uint32_t bits)
     return e > -126 ? e : -126;
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+
+// Partial results of attention whose keys are split over workgroups: for every row and split {maximum in units of log2,
+// sum of weights} and 128 weighted sums of values.  A split without keys has sum 0, and its sums may hold
+// anything.
+//
+// A kernel of its own joins them (cache_merge.hip), or, in small calls, the workgroup that arrives last: that saves a launch.
+// Its reads have to see what workgroups on other dies wrote: there, partial results are written and read with
+// device-wide (relaxed atomic) accesses, which no die's cache holds back, and every wavefront waits for its writes
+// before its workgroup counts itself as arrived.  (A release fence would write back all of the die's cache instead, once
+// a workgroup.)  A counter is 0 between calls.
+struct Partials {
+    unsigned long long* ml;             // [rows][nsplit] float2
+    unsigned long long* acc;            // [rows][nsplit][64] float2
+    uint32_t* arrived;                  // of each group of rows, kArrivedStride apart; null: another kernel joins
+};
+
+__device__ __forceinline__ void put_pair(unsigned long long* p, float x, float y)
+{
+    __hip_atomic_store(p, static_cast<unsigned long long>(__float_as_uint(y)) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ f32x2 get_pair(const unsigned long long* p)
+{
+    return __builtin_bit_cast(f32x2, __hip_atomic_load(const_cast<unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+}
+
+// One workgroup's part: a pair of columns of a row, and the row's maximum and sum.
+__device__ __forceinline__ void put_part(const Partials& p, size_t at, uint32_t pair, float m, float l, f32x2 a)
+{
+    if (p.arrived) {
+        put_pair(p.acc + at * 64 + pair, a.x, a.y);
+        if (pair == 0) put_pair(p.ml + at, m, l);
+    } else {
+        reinterpret_cast<f32x2*>(p.acc)[at * 64 + pair] = a;
+        if (pair == 0) reinterpret_cast<f32x2*>(p.ml)[at] = f32x2{m, l};
+    }
+}
+
+// Counts the workgroup as arrived once its writes are done; true for the last of them.
+__device__ __forceinline__ bool arrives_last(uint32_t* arrived, uint32_t nsplit, uint32_t* lds)
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const uint32_t before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (before == nsplit - 1) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        *lds = before;
+    }
+    __syncthreads();
+    asm volatile("" ::: "memory");
+    return *lds == nsplit - 1;
+}
+
+// A running softmax sum of partial results.
+struct Join {
+    float m = -INFINITY, l = 0.0f;
+    f32x2 a = {0.0f, 0.0f};
+    __device__ __forceinline__ void add(f32x2 ml, f32x2 v)
+    {
+        if (ml.y == 0.0f) return;
+        const float mn = fmaxf(m, ml.x);
+        const float fo = l != 0.0f ? __builtin_amdgcn_exp2f(m - mn) : 0.0f, fn = __builtin_amdgcn_exp2f(ml.x - mn);
+        a.x = __builtin_fmaf(a.x, fo, fn * v.x);
+        a.y = __builtin_fmaf(a.y, fo, fn * v.y);
+        l = __builtin_fmaf(l, fo, fn * ml.y);
+        m = mn;
+    }
+};
+
+// Joins the partial results of rows row0 .. row0 + rows - 1 into out, in the workgroup that arrived last.  A group of 64
+// threads has a row, two columns a thread, and NB splits on their way at once; where there are fewer rows than groups,
+// the groups share out each row's splits and are joined in order.  `lds`: 128 f32x2 for each group but the first.
+template <int NT, uint32_t NB>
+__device__ __forceinline__ void join_rows(const Partials& p, uint32_t row0, uint32_t rows, uint32_t nsplit, float* out, f32x2* lds)
+{
+    constexpr uint32_t GROUPS = NT / 64;
+    const uint32_t c = threadIdx.x & 63, group = threadIdx.x >> 6;
+    f32x2* o = reinterpret_cast<f32x2*>(out);
+    const bool alone = rows >= GROUPS;                    // a group has its rows to itself
+    const uint32_t stride = alone ? 1 : GROUPS;
+    for (uint32_t r = alone ? group : 0; r < rows; r += alone ? GROUPS : 1) {
+        Join j;
+        for (uint32_t s = alone ? 0 : group; s < nsplit; s += stride * NB) {
+            f32x2 ml[NB], v[NB];
+#pragma unroll
+            for (uint32_t y = 0; y < NB; ++y) {
+                const size_t at = static_cast<size_t>(row0 + r) * nsplit + min(s + stride * y, nsplit - 1);
+                ml[y] = get_pair(p.ml + at);
+                v[y] = get_pair(p.acc + at * 64 + c);
+            }
+#pragma unroll
+            for (uint32_t y = 0; y < NB; ++y)
+                if (s + stride * y < nsplit) j.add(ml[y], v[y]);
+        }
+        if (!alone) {
+            __syncthreads();
+            if (group > 0) {
+                f32x2* to = lds + (group - 1) * 128;
+                to[c] = f32x2{j.m, j.l};
+                to[64 + c] = j.a;
+            }
+            __syncthreads();
+            if (group > 0) continue;
+#pragma unroll
+            for (uint32_t k = 0; k + 1 < GROUPS; ++k) j.add(lds[k * 128 + c], lds[k * 128 + 64 + c]);
+        }
+        o[static_cast<size_t>(row0 + r) * 64 + c] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
+    }
+}
 
 #endif   // __HIPCC__
 

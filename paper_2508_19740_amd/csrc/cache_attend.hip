@@ -1,5 +1,4 @@
-// Attention over gathered rows of the 8-bit cache, and the merge of partial results that it shares with
-// attention over the whole cache.
+// Attention over gathered rows of the 8-bit cache.
 //
 // As in attend.hip, the k rows of a query head are split over workgroups, a wavefront issues the loads of
 // all its rows before it uses any (random rows: bound by the latency and bandwidth of memory), and
@@ -15,6 +14,7 @@ namespace {
 constexpr int kLanes = 8;               // lanes of a row
 constexpr int kElems = 16;              // elements of a lane
 constexpr int kRowsPerLoad = 64 / kLanes;
+constexpr int kWholeThreads = 1024;     // threads of a workgroup that takes a whole head
 constexpr float kLog2e = 1.4426950408889634f;
 
 // 16 bytes of a row that is used once: the rows of a step do not fit into a cache
@@ -51,6 +51,19 @@ __device__ __forceinline__ float add_across_row(float x)
     return x;
 }
 
+// Lanes below 32 get a summed over the two halves of the wavefront, the others b.
+__device__ __forceinline__ float add_halves(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+// The same over the two quarters of each half: lanes with bit 4 clear get a, the others b.
+__device__ __forceinline__ float add_quarters(float a, float b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 __device__ __forceinline__ void load_q(const bf16_raw* q, float (&o)[kElems])
 {
     const uint4* s = reinterpret_cast<const uint4*>(q);
@@ -82,8 +95,7 @@ struct AttendArgs {
     const float* k_scale;
     const float* v_scale;
     const int32_t* idx;
-    float2* part_ml;
-    float* part_acc;
+    Partials part;
     float* out;
     int64_t Nmax, blocks;
     int topk, Hq, Hkv, nsplit, shift;
@@ -97,10 +109,12 @@ __global__ __launch_bounds__(NT) void cache_attend_kernel(AttendArgs a)
     constexpr int NW = NT / 64;
     constexpr int RPW = RB / NW;
     constexpr int ITERS = RPW / kRowsPerLoad;
+    constexpr bool JOINS = NT == kThreads && RB == kAttendMinRows;   // small calls: few heads and rows
     static_assert(ITERS >= 1 && RPW % kRowsPerLoad == 0, "row tiling");
 
     __shared__ float s_m[NW], s_l[NW];
-    __shared__ float s_acc[NW][kHeadDim];
+    __shared__ float s_acc[JOINS ? 2 * NW : NW][kHeadDim];     // twice: the join's
+    __shared__ uint32_t s_before;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int split = blockIdx.x;
@@ -176,110 +190,42 @@ __global__ __launch_bounds__(NT) void cache_attend_kernel(AttendArgs a)
 #pragma unroll
         for (int e = 0; e < kElems; ++e) acc[e] = __builtin_fmaf(pv, f[e], acc[e]);
     }
+    // Sums over the eight rows of a load.  Halves of the wavefront, then of each half, exchange half of what they hold, so
+    // that each lane ends with a quarter of its elements, summed over four rows; then neighbours of eight lanes.
 #pragma unroll
-    for (int off = kLanes; off < 64; off <<= 1) {
-        l += __shfl_xor(l, off);
+    for (int off = kLanes; off < 64; off <<= 1) l += __shfl_xor(l, off);
+    float part[4];
+    {
+        float a8[8];
 #pragma unroll
-        for (int e = 0; e < kElems; ++e) acc[e] += __shfl_xor(acc[e], off);
+        for (int e = 0; e < 8; ++e) a8[e] = add_halves(acc[e], acc[e + 8]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[e] = add_quarters(a8[e], a8[e + 4]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part[e] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(part[e]), 0x128, 0xf, 0xf, true));   // row_ror:8
     }
-    if (grp == 0) {
-#pragma unroll
-        for (int e = 0; e < kElems; ++e) s_acc[wave][sub * kElems + e] = acc[e];
-    }
+    // lane 32h + 16q + s (s < 8) has elements 8h + 4q .. + 3 of lane s's sixteen
+    if ((lane & 8) == 0)
+        *reinterpret_cast<float4*>(&s_acc[wave][sub * kElems + (lane >> 5) * 8 + (lane >> 4 & 1) * 4]) = make_float4(part[0], part[1], part[2], part[3]);
     if (lane == 0) { s_m[wave] = m; s_l[wave] = l; }
     __syncthreads();
 
-    // merge the waves; thread c < 128 owns output column c.  A wave without rows has l = 0.
-    if (tid < kHeadDim) {
-        float M = s_m[0];
+    // merge the waves; thread c < 64 owns output columns 2c and 2c + 1
+    if (wave == 0) {
+        Join j;
 #pragma unroll
-        for (int w = 1; w < NW; ++w) M = fmaxf(M, s_m[w]);
-        float o = 0.0f, lsum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            if (s_l[w] != 0.0f) {
-                const float f = __builtin_amdgcn_exp2f(s_m[w] - M);
-                o = __builtin_fmaf(f, s_acc[w][tid], o);
-                lsum = __builtin_fmaf(f, s_l[w], lsum);
-            }
-        }
-        if (a.nsplit == 1) {   // the whole head is here
-            a.out[bh * kHeadDim + tid] = lsum != 0.0f ? o / lsum : 0.0f;
-            return;
-        }
-        const int64_t pi = bh * a.nsplit + split;
-        a.part_acc[pi * kHeadDim + tid] = o;
-        if (tid == 0) a.part_ml[pi] = make_float2(M, lsum);
-    }
-}
-
-// Merge of a row's partial results {maximum in units of log2, sum} and accumulators.  32 threads, with four columns
-// each, fold the splits part, part + PARTS, ... of a row with a running maximum, up to eight loads ahead of the
-// arithmetic; the row's PARTS groups of them are then combined in order.  A split without rows has sum 0 and is left
-// out: its accumulator may hold anything.
-template <int PARTS>
-__global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __restrict__ part_ml, const float4* __restrict__ part_acc,
-                                                               float4* __restrict__ out, int64_t rows, int nsplit)
-{
-    constexpr int NB = 8, QUADS = kHeadDim / 4, RPW = kThreads / QUADS / PARTS;   // rows of a workgroup
-    __shared__ float s_m[PARTS][kThreads / PARTS], s_l[PARTS][kThreads / PARTS];
-    __shared__ float4 s_a[PARTS][kThreads / PARTS];
-    const int tid = threadIdx.x;
-    const int c = tid % QUADS, part = tid / QUADS % PARTS, slot = tid / (QUADS * PARTS);
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * RPW + slot;
-    const int64_t at = min(row, rows - 1) * nsplit;       // threads behind the last row repeat it
-    float m = -INFINITY, l = 0.0f;
-    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int s0 = part; s0 < nsplit; s0 += PARTS * NB) {
-        float2 v[NB];
-        float4 av[NB];
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            const int sp = s0 + PARTS * i;
-            const int64_t spc = at + (sp < nsplit ? sp : s0);      // in-bounds stand-in, left out below
-            v[i] = part_ml[spc];
-            av[i] = part_acc[spc * QUADS + c];
-            if (sp >= nsplit) v[i].y = 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-            if (v[i].y != 0.0f) {
-                const float mn = fmaxf(m, v[i].x);
-                const float fo = l != 0.0f ? __builtin_amdgcn_exp2f(m - mn) : 0.0f, fn = __builtin_amdgcn_exp2f(v[i].x - mn);
-                a.x = __builtin_fmaf(a.x, fo, fn * av[i].x);
-                a.y = __builtin_fmaf(a.y, fo, fn * av[i].y);
-                a.z = __builtin_fmaf(a.z, fo, fn * av[i].z);
-                a.w = __builtin_fmaf(a.w, fo, fn * av[i].w);
-                l = __builtin_fmaf(l, fo, fn * v[i].y);
-                m = mn;
-            }
+        for (int w = 0; w < NW; ++w) j.add(f32x2{s_m[w], s_l[w]}, reinterpret_cast<const f32x2*>(s_acc[w])[lane]);
+        if (NT == kWholeThreads) {   // the whole head is here
+            reinterpret_cast<f32x2*>(a.out + bh * kHeadDim)[lane] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
+        } else {
+            put_part(a.part, bh * a.nsplit + split, lane, j.m, j.l, j.a);
         }
     }
-    if constexpr (PARTS > 1) {
-        const int e = slot * QUADS + c;
-        s_m[part][e] = m; s_l[part][e] = l; s_a[part][e] = a;
-        __syncthreads();
-        if (part != 0) return;
-        m = -INFINITY;
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) m = fmaxf(m, s_m[p][e]);
-        l = 0.0f;
-        a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            if (s_l[p][e] != 0.0f) {
-                const float f = __builtin_amdgcn_exp2f(s_m[p][e] - m);
-                const float4 o = s_a[p][e];
-                a.x = __builtin_fmaf(f, o.x, a.x);
-                a.y = __builtin_fmaf(f, o.y, a.y);
-                a.z = __builtin_fmaf(f, o.z, a.z);
-                a.w = __builtin_fmaf(f, o.w, a.w);
-                l = __builtin_fmaf(f, s_l[p][e], l);
-            }
-        }
+    if constexpr (JOINS) {
+        if (!a.part.arrived) return;
+        if (arrives_last(a.part.arrived + bh * kArrivedStride, static_cast<uint32_t>(a.nsplit), &s_before))
+            join_rows<NT, 16>(a.part, static_cast<uint32_t>(bh), 1, static_cast<uint32_t>(a.nsplit), a.out, reinterpret_cast<f32x2*>(&s_acc[0][0]));
     }
-    if (row >= rows) return;
-    out[row * QUADS + c] = l != 0.0f ? make_float4(a.x / l, a.y / l, a.z / l, a.w / l) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 
 template <typename CT, typename QT, int RB, int NT = kThreads>
@@ -287,6 +233,8 @@ void launch_rb(spotlight_ctx* ctx, StageTimer& timer, AttendArgs& a)
 {
     const Plan& p = ctx->plan;
     a.nsplit = (a.topk + RB - 1) / RB;
+    if (NT == kWholeThreads || RB != kAttendMinRows || !joins_in_place(static_cast<int64_t>(p.B) * p.Hq, 1, a.nsplit)) a.part.arrived = nullptr;
+    if (timer.rec) timer.rec->whole = NT == kWholeThreads || a.part.arrived;
     timer.launch(cache_attend_kernel<CT, QT, RB, NT>, dim3(static_cast<unsigned>(a.nsplit), static_cast<unsigned>(p.B * p.Hq)), dim3(NT), 0, a);
 }
 
@@ -297,32 +245,18 @@ int launch_t(spotlight_ctx* ctx, AttendArgs& a)
     const int64_t heads = static_cast<int64_t>(p.B) * p.Hq;
     {
         StageTimer timer(ctx, SPOTLIGHT_STAGE_ATTEND);
-        if (a.topk <= 256) {
-            if (timer.rec) timer.rec->whole = true;
-            if (a.topk <= 128) launch_rb<CT, QT, 128, 1024>(ctx, timer, a);
-            else launch_rb<CT, QT, 256, 1024>(ctx, timer, a);
-            return hip_rc(hipGetLastError());
-        }
-        if (heads * ((a.topk + 127) / 128) >= 1024) launch_rb<CT, QT, 128>(ctx, timer, a);
+        if (a.topk <= 128) launch_rb<CT, QT, 128, kWholeThreads>(ctx, timer, a);
+        else if (a.topk <= 256) launch_rb<CT, QT, 256, kWholeThreads>(ctx, timer, a);
+        else if (heads * ((a.topk + 127) / 128) >= 1024) launch_rb<CT, QT, 128>(ctx, timer, a);
         else if (heads * ((a.topk + 63) / 64) >= 1024) launch_rb<CT, QT, 64>(ctx, timer, a);
         else launch_rb<CT, QT, 32>(ctx, timer, a);
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
-    return launch_cache_merge(ctx, a.part_ml, a.part_acc, heads, a.nsplit, a.out);
+    if (a.nsplit == 1 || a.part.arrived) return SPOTLIGHT_OK;
+    return launch_cache_merge(ctx, a.part.ml, a.part.acc, heads, a.nsplit, a.out);
 }
 
 }  // namespace
-
-int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const float* part_acc, int64_t rows, int nsplit, float* out)
-{
-    StageTimer timer(ctx, SPOTLIGHT_STAGE_MERGE);
-    // few splits: a row's are folded by the same threads, and a workgroup has eight rows
-    const bool few = nsplit <= 8;
-    const int64_t per = few ? kThreads / (kHeadDim / 4) : 1;
-    timer.launch(few ? cache_merge_kernel<1> : cache_merge_kernel<8>, dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kThreads), 0,
-                 static_cast<const float2*>(part_ml), reinterpret_cast<const float4*>(part_acc), reinterpret_cast<float4*>(out), rows, nsplit);
-    return hip_rc(hipGetLastError());
-}
 
 int launch_cache_attend(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, const int32_t* idx, int k, float scale, float* out)
 {
@@ -334,8 +268,9 @@ int launch_cache_attend(spotlight_ctx* ctx, const void* q, const spotlight_cache
     a.k_scale = c.k_scale;
     a.v_scale = c.v_scale;
     a.idx = idx;
-    a.part_ml = reinterpret_cast<float2*>(ctx->workspace + p.off_part_ml);
-    a.part_acc = reinterpret_cast<float*>(ctx->workspace + p.off_part_acc);
+    a.part.ml = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_part_ml);
+    a.part.acc = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_part_acc);
+    a.part.arrived = reinterpret_cast<uint32_t*>(ctx->workspace + p.off_arrived);
     a.out = out;
     a.Nmax = p.Nmax;
     a.blocks = (p.Nmax + c.block_tokens - 1) / c.block_tokens;

@@ -18,13 +18,15 @@
 //
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
-//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).
+//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (20 bits).
 //   p   is in [0, 16], scaled by 2^11 and split in two parts: 20 bits, or 2^-35 where that is more.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
 //       ratio is above 2^-20, and at most 2^-30 of the largest block's size off below.
 //
 // A row reads 256 bytes a key and key-value head, whatever G and n_q: with few rows the kernel is bound by
 // memory.  The keys are split over workgroups, and a merge joins them.
+#include <algorithm>
+
 #include "cache.h"
 
 namespace spotlight {
@@ -100,26 +102,6 @@ template <> struct Operand<I8> {
     }
 };
 
-struct DenseArgs {
-    const void* q;
-    const uint8_t* k;
-    const uint8_t* v;
-    const float* k_scale;
-    const float* v_scale;
-    const int32_t* lens;
-    float2* part_ml;
-    float* part_acc;
-    float* out;
-    int64_t Nmax, blocks, n_tokens;
-    int64_t chunk;                      // keys of a split, a multiple of kStep * kWaves
-    uint32_t rows, n_q;                 // rows of a key-value head: G * n_q
-    uint32_t nsplit;
-    uint32_t turn;                      // by how much the splits of one head are turned against the last one's
-    int Hkv, shift;
-    float scale2;                       // |scale| * log2(e)
-    bool negate;                        // the scale is negative: q is negated
-};
-
 // x less the low or the high half of h, in one instruction.
 __device__ __forceinline__ float less_low(float x, h2 h)
 {
@@ -134,6 +116,25 @@ __device__ __forceinline__ float less_high(float x, h2 h)
     return d;
 }
 
+struct DenseArgs {
+    const void* q;
+    const uint8_t* k;
+    const uint8_t* v;
+    const float* k_scale;
+    const float* v_scale;
+    const int32_t* lens;
+    Partials part;
+    float* out;
+    int64_t Nmax, blocks, n_tokens;
+    int64_t chunk;                      // keys of a split, a multiple of kStep * kWaves
+    uint32_t rows, n_q;                 // rows of a key-value head: G * n_q
+    uint32_t nsplit;
+    uint32_t turn;                      // by how much the splits of one head are turned against the last one's
+    int Hkv, shift;
+    float scale2;                       // |scale| * log2(e)
+    bool negate;                        // the scale is negative: q is negated
+};
+
 template <bool B> struct Flag { static constexpr bool value = B; };
 
 __device__ __forceinline__ float across_groups_max(float x)
@@ -147,43 +148,60 @@ __device__ __forceinline__ float across_groups_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// One row's 32 elements of a lane, scaled by 2^(13 - exponent of the row's largest) and split into QP
-// binary16 parts, negated if asked; returns minus the exponent that was put in.
+// One row's 32 elements of a lane, scaled by a power of two that brings the row's largest into [2^13, 2^14), negated if
+// asked and split into QP binary16 parts; returns the exponent that takes the scaling back.
 template <typename QT, int QP>
 __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP][4])
 {
-    float x[32];
+    constexpr int NV = 32 * sizeof(QT) / 16;
+    uint4 u[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) u[i] = reinterpret_cast<const uint4*>(q)[i];
+    uint32_t most = 0;                           // bits of the largest magnitude
     if constexpr (sizeof(QT) == 2) {
-        const uint4* s = reinterpret_cast<const uint4*>(q);
+        typedef uint16_t us2 __attribute__((ext_vector_type(2)));
+        us2 top = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 u = s[i];
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { x[8 * i + 2 * j] = __uint_as_float(w[j] << 16); x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(us2, w[j] & 0x7fff7fffu));
         }
+        most = static_cast<uint32_t>(max(top.x, top.y)) << 16;
     } else {
-        const float4* s = reinterpret_cast<const float4*>(q);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 u = s[i];
-            x[4 * i] = u.x; x[4 * i + 1] = u.y; x[4 * i + 2] = u.z; x[4 * i + 3] = u.w;
-        }
+        for (int i = 0; i < NV; ++i)
+            most = max(max(max(most, u[i].x & 0x7fffffffu), u[i].y & 0x7fffffffu), max(u[i].z & 0x7fffffffu, u[i].w & 0x7fffffffu));
     }
-    float most = 0.0f;
+    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
+    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
+    // rows below 2^-113 are scaled as those at it; an infinity or a NaN makes the row's results NaN, however it is scaled
+    const int ex = min(max(static_cast<int>(most >> 23) - 127, -113), 127);
+    const float up = __uint_as_float(static_cast<uint32_t>(13 - ex + 127) << 23 | (negate ? 0x80000000u : 0u));
 #pragma unroll
-    for (int i = 0; i < 32; ++i) most = fmaxf(most, fabsf(x[i]));
-    most = across_groups_max(most);
-    const int ex = (most > 0.0f && most < INFINITY) ? ilogbf(most) : 0;
+    for (int c = 0; c < 4; ++c) {
+        h2 hi[4], lo[4];
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float y = ldexpf(negate ? -x[8 * c + j] : x[8 * c + j], 13 - ex);
-            const _Float16 hi = static_cast<_Float16>(y);
-            frag[0][c][j] = hi;
-            if constexpr (QP == 2) frag[1][c][j] = static_cast<_Float16>(y - static_cast<float>(hi));
+        for (int j = 0; j < 4; ++j) {
+            float x, y;
+            if constexpr (sizeof(QT) == 2) {
+                const uint32_t w = j == 0 ? u[c].x : j == 1 ? u[c].y : j == 2 ? u[c].z : u[c].w;
+                x = __uint_as_float(w << 16);
+                y = __uint_as_float(w & 0xffff0000u);
+            } else {
+                const uint4 w = u[2 * c + j / 2];
+                x = __uint_as_float(j % 2 ? w.z : w.x);
+                y = __uint_as_float(j % 2 ? w.w : w.y);
+            }
+            x *= up;
+            y *= up;
+            hi[j] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+            lo[j] = hi[j];
+            if constexpr (QP == 2) lo[j] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(less_low(x, hi[j]), less_high(y, hi[j])));
         }
+        frag[0][c] = join(hi[0], hi[1], hi[2], hi[3]);
+        if constexpr (QP == 2) frag[1][c] = join(lo[0], lo[1], lo[2], lo[3]);
+    }
     return ex - 13;
 }
 
@@ -195,6 +213,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     typedef Operand<CT> Op;
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     __shared__ float s_acc[kWaves][16][kHeadDim + 4];
+    __shared__ uint32_t s_before;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, i = lane & 15;
@@ -446,29 +465,23 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
                     f4{acc[t][d][r], acc[t][d + 1][r], acc[t][d + 2][r], acc[t][d + 3][r]} * to_value;
         __syncthreads();
         const int left = static_cast<int>(a.rows - min(r0 + 16 * t, a.rows));
-        for (int e = tid; e < 16 * kHeadDim && e / kHeadDim < left; e += kThreads) {
-            const int row = e / kHeadDim, col = e % kHeadDim;
-            float M = -INFINITY;
+        for (int e = tid; e < 16 * 64 && e / 64 < left; e += kThreads) {
+            const int row = e / 64, pair = e % 64;
+            Join j;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][row]);
-            float o = 0.0f, lsum = 0.0f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                if (s_l[w][row] != 0.0f) {
-                    const float f = __builtin_amdgcn_exp2f(s_m[w][row] - M);
-                    o = __builtin_fmaf(f, s_acc[w][row][col], o);
-                    lsum = __builtin_fmaf(f, s_l[w][row], lsum);
-                }
-            }
-            const int64_t at = head * a.rows + r0 + 16 * t + row;
+            for (int w = 0; w < kWaves; ++w) j.add(f32x2{s_m[w][row], s_l[w][row]}, reinterpret_cast<const f32x2*>(s_acc[w][row])[pair]);
+            const size_t at = head * a.rows + r0 + 16 * t + row;
             if (a.nsplit == 1) {
-                a.out[at * kHeadDim + col] = lsum != 0.0f ? o / lsum : 0.0f;
+                reinterpret_cast<f32x2*>(a.out + at * kHeadDim)[pair] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
             } else {
-                a.part_acc[(at * a.nsplit + split) * kHeadDim + col] = o;
-                if (col == 0) a.part_ml[at * a.nsplit + split] = make_float2(M, lsum);
+                put_part(a.part, at * a.nsplit + split, pair, j.m, j.l, j.a);
             }
         }
     }
+    if (a.nsplit == 1 || !a.part.arrived) return;
+    const uint32_t tiles = gridDim.x / a.nsplit;
+    if (arrives_last(a.part.arrived + (blockIdx.y * tiles + blockIdx.x / a.nsplit) * kArrivedStride, a.nsplit, &s_before))
+        join_rows<kThreads, 16>(a.part, static_cast<uint32_t>(head) * a.rows + r0, min(16u * MT, a.rows - r0), a.nsplit, a.out, reinterpret_cast<f32x2*>(&s_acc[0][0][0]));
 }
 
 template <typename CT, typename QT>
@@ -497,8 +510,8 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     a.k_scale = c.k_scale;
     a.v_scale = c.v_scale;
     a.lens = lens;
-    a.part_ml = reinterpret_cast<float2*>(ctx->workspace + p.off_dense_ml);
-    a.part_acc = reinterpret_cast<float*>(ctx->workspace + p.off_dense_acc);
+    a.part.ml = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_dense_ml);
+    a.part.acc = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_dense_acc);
     a.out = out;
     a.Nmax = p.Nmax;
     a.blocks = (p.Nmax + c.block_tokens - 1) / c.block_tokens;
@@ -515,9 +528,12 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     if (rc != SPOTLIGHT_OK) return rc;
     a.chunk = sp.chunk;
     a.nsplit = static_cast<uint32_t>(sp.nsplit);
+    const int64_t groups = static_cast<int64_t>(p.B) * p.Hkv * ((a.rows + 16 * sp.tiles - 1) / (16 * sp.tiles));
+    a.part.arrived = joins_in_place(groups, std::min<int64_t>(a.rows, 16 * sp.tiles), sp.nsplit) ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_arrived) : nullptr;
+    const bool done = sp.nsplit == 1 || a.part.arrived;       // nothing is left to merge
     {
         StageTimer timer(ctx, SPOTLIGHT_STAGE_ATTEND);
-        if (timer.rec) timer.rec->whole = a.nsplit == 1;
+        if (timer.rec) timer.rec->whole = done;
         if (p.kv_dtype == SPOTLIGHT_BF16) {
             if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, bf16_raw>(ctx, timer, a, sp.tiles);
             else launch_mt<I8, bf16_raw>(ctx, timer, a, sp.tiles);
@@ -527,8 +543,8 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
         }
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
-    if (a.nsplit == 1) return SPOTLIGHT_OK;
-    return launch_cache_merge(ctx, a.part_ml, a.part_acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, sp.nsplit, out);
+    if (done) return SPOTLIGHT_OK;
+    return launch_cache_merge(ctx, a.part.ml, a.part.acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, sp.nsplit, out);
 }
 
 }  // namespace spotlight

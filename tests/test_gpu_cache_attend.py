@@ -282,3 +282,27 @@ def test_a_graph_and_stages():
     ctx.profile_enable(False)
     assert prof["attend"][1] == 1 and prof["merge"][1] == 1
     ctx.close()
+
+
+@pytest.mark.parametrize("hq,hkv,n,nq", [(1, 1, 2000, 1), (8, 8, 1000, 1), (4, 1, 1500, 1), (2, 2, 4000, 1), (1, 1, 700, 9)])
+def test_small_calls_one_after_the_other(hq, hkv, n, nq):
+    """Small calls, whose last workgroup joins the parts of the others: results do not depend on what the workspace held, however
+    calls of other inputs, shapes and kinds follow each other."""
+    host = cc.random_cache(1, hkv, n, 64, "e4m3", 21)
+    ctx, cache = _ctx(1, hq, hkv, n, 512), host.device()
+    qs = [_q(i, "bf16", 1, hq, nq, size=2.0).to(DEV) for i in range(4)]
+    idx = torch.randint(0, n, (1, hq, 500), dtype=torch.int32, generator=torch.Generator().manual_seed(3)).to(DEV)
+    lens = [torch.tensor([v], dtype=torch.int32, device=DEV) for v in (n, n // 3, 1, 0)]
+    calls = [lambda q=q, ln=ln: ctx.dense_decode_cache(q, cache, n, ln) for q in qs for ln in lens]
+    calls += [lambda q=q: ctx.sparse_decode_cache(q[:, :, 0].contiguous(), cache, idx) for q in qs]
+    first = []
+    for c in calls:
+        first.append(c())
+        torch.cuda.synchronize()
+    order = torch.randint(0, len(calls), (600,), generator=torch.Generator().manual_seed(5)).tolist()
+    got = [calls[i]() for i in order]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, first[i]) for g, i in zip(got, order))
+    want, mag, size = _dense(host, qs[1].cpu(), n, None, 0, 0, hq // hkv, nq)
+    _check(first[4][0, 0], want, cc.tolerance(mag, size, 32 + n // 8, 1, 2.0 ** -20) + cc.split_floor(host.values("v")[0, 0]), "first")
+    ctx.close()
