@@ -67,12 +67,14 @@ int make_plan(const spotlight_config* c, Plan* p)
     p->off_operands = off;  off = align_up(off + wheads * screen_operand_bytes(p->hidden, p->W), 256);
     p->off_open = off;      off = align_up(off + kheads * ((p->Nmax + 31) / 32) * 4, 256);
     p->off_open_counts = off; off = align_up(off + kheads * ((p->Nmax + 65535) / 65536) * 128, 256);
-    // Partial results of attention over the whole 8-bit cache.  Sixteen thousand rows: 256 workgroups of 64
-    // rows, or eight splits for each of 256 workgroups of eight; fewer where the cache cannot be split that far.
-    const int64_t most_rows = static_cast<int64_t>(BH) * ((p->Nmax + 127) / 128) * 8;
-    p->dense_rows = most_rows < 16384 ? most_rows : 16384;
+    // Partial results of attention over the whole 8-bit cache: enough for 512 workgroups of 32 rows, or 1024 of 16, and
+    // for every query twice; fewer where the cache cannot be split that far.
+    const int64_t whole = static_cast<int64_t>(BH), least = 2 * whole, most = whole * ((p->Nmax + 127) / 128) * 8;
+    p->dense_rows = most < 16384 ? most : 16384;
+    if (p->dense_rows < least) p->dense_rows = least;
     p->off_dense_ml = off;  off = align_up(off + static_cast<size_t>(p->dense_rows) * 8, 256);
     p->off_dense_acc = off; off = align_up(off + static_cast<size_t>(p->dense_rows) * kHeadDim * 4, 256);
+    p->off_runs = off;      off = align_up(off + static_cast<size_t>(p->B) * 8, 256);
     p->off_arrived = off;   off = align_up(off + kArrivedBytes, 256);
     p->off_audit = off;     off = align_up(off + sizeof(AuditRec), 256);
     p->total_bytes = off;

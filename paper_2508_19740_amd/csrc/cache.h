@@ -10,46 +10,67 @@
 namespace spotlight {
 namespace cache {
 
-// How attention over the whole cache is shared out (host): tiles of 16 rows a workgroup, and the keys of a
-// split.  Partial results of all rows and splits fit the workspace's dense_rows, and a split's keys are
-// a multiple of its wavefronts' steps.
-constexpr int kDenseStep = 32, kDenseWaves = 4;
-constexpr int64_t kDenseMostKeys = 1 << 25;   // of a split: a wavefront's quarter of them stays below 2^31 bytes
-struct DenseSplit {
-    int tiles, nsplit;
-    int64_t chunk;
+// Division of numbers below 2^31 by one that the host knows.
+struct FastDiv {
+    uint32_t d, mul, shift;
+#if defined(__HIPCC__)
+    __device__ __forceinline__ uint32_t over(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+#endif
 };
-inline int split_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, DenseSplit* s)
+inline FastDiv fast_div(uint32_t d)
 {
-    const int64_t rows = static_cast<int64_t>(p.G) * n_q, heads = static_cast<int64_t>(p.B) * p.Hkv;
-    if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;   // a grid's first dimension, and 32 bits for a row
-    s->tiles = rows <= 16 ? 1 : 2;
-    const int64_t groups = heads * ((rows + 16 * s->tiles - 1) / (16 * s->tiles));
-    constexpr int64_t unit = kDenseStep * kDenseWaves;
-    const int64_t room = p.dense_rows / (heads * rows), most = (n_tokens + unit - 1) / unit;
-    int64_t n = (static_cast<int64_t>(n_cus) * (s->tiles == 2 ? 2 : 4) + groups - 1) / groups;
-    if (n > room) n = room;
-    if (n > most) n = most;
-    if (n < 1) n = 1;
-    if (n_tokens > n * kDenseMostKeys) {
-        n = (n_tokens + kDenseMostKeys - 1) / kDenseMostKeys;
-        if (n > room) return SPOTLIGHT_ERR_UNSUPPORTED;
-    }
-    s->chunk = ((n_tokens + n - 1) / n + unit - 1) / unit * unit;
-    s->nsplit = static_cast<int>((n_tokens + s->chunk - 1) / s->chunk);
-    return SPOTLIGHT_OK;
+    FastDiv f{d, 0, 0};
+    while (f.shift < 31 && (1u << f.shift) < d) ++f.shift;
+    f.mul = static_cast<uint32_t>((((1ull << f.shift) - d) << 32) / d + 1);
+    return f;
 }
+
+// How attention over the whole cache is shared out.  A workgroup has a tile of rows of a key-value head and a run of
+// keys, counted in units of 128.  Sequences of one length are split alike.  Where each has a length of its own, which the
+// host does not know, the kernel takes runs of one size for all, about the smallest with which all sequences make no
+// more than `most_runs`, so that every workgroup has about as much to do.  (Runs of a fixed part of
+// n_tokens leave compute units idle: 16 sequences of 2049 .. 32769 tokens, 28 / 4 heads, 69 -> 62 us.)
+constexpr int kDenseStep = 32, kDenseWaves = 4, kDenseUnit = kDenseStep * kDenseWaves;
+constexpr int64_t kDenseMostKeys = 1 << 25;   // of a workgroup: a wavefront's quarter of them stays below 2^31 bytes
+struct DenseShares {
+    const int32_t* lens;
+    uint32_t batch, units;      // units of n_tokens
+    uint32_t chunk;             // units of a run, and
+    uint32_t nsplit;            // runs of a sequence, without lens
+    uint32_t most_runs;         // with lens: runs of all sequences, at least twice as many as there are sequences; 0: a run is a sequence
+    uint32_t tile_rows;         // rows of a workgroup's partial result
+    uint32_t tiles;             // tiles of rows of a key-value head
+    FastDiv by_nsplit, by_most, by_spare, by_heads, by_tiles8;    // by_spare: most_runs - batch
+};
+struct DensePlan {
+    DenseShares shares;
+    int row_tiles;              // of 16 rows, a workgroup
+    uint32_t grid;              // workgroups, at most
+    int64_t about;              // runs of a sequence, on average
+    bool splits, joins;         // whether there are partial results, and whether the last workgroup joins them
+};
+int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d);
 
 // Whether the last workgroup of each group of rows joins its partial results, instead of a launch of its own: small
 // calls, where the join is one round of loads (about 2 us, since nothing of it is in a cache; a launch takes 3.5 us of the
 // host).  Against the merge kernel, called back to back: 1 head, 600 / 4096 / 8192 tokens 10.6 / 11.5 / 11.5 -> 8.7 / 8.4 /
 // 8.8 us, gathered 300 / 2000 of them 10.2 / 10.4 -> 7.8 / 7.7 us, and no slower in a graph; with two rounds, 16384
 // tokens 11.3 -> 11.2 us (graph 10.2 -> 11.2), 1000 tokens of 4 groups of 8, 11.6 -> 10.5 us (graph 9.0 -> 10.4).
-inline bool joins_in_place(int64_t groups, int64_t rows, int64_t nsplit)
+inline bool joins_in_place(int64_t workgroups, int64_t rows, int64_t nsplit)
 {
     const int64_t rounds = rows >= 4 ? (rows + 3) / 4 * ((nsplit + 15) / 16) : rows * ((nsplit + 63) / 64);
-    return nsplit > 1 && rounds <= 1 && groups * nsplit <= kJoinGroups;
+    return nsplit > 1 && rounds <= 1 && workgroups <= kJoinGroups;
 }
+
+// The rows that the merge kernel joins: nsplit partial results each, one after the other; or (runs set) those of attention
+// over the whole cache, where the runs of a sequence lie apart.
+struct MergeRows {
+    int64_t rows;
+    int nsplit;
+    const uint2* runs;          // [batch] {first, number}
+    FastDiv by_rows, by_heads, by_tile;
+    uint32_t tiles, tile_rows;
+};
 
 #if defined(__HIPCC__)
 
@@ -156,6 +177,97 @@ __device__ __forceinline__ bool arrives_last(uint32_t* arrived, uint32_t nsplit,
     return *lds == nsplit - 1;
 }
 
+// What a run of keys belongs to: its sequence, which run of it, how many there are, and the first one's number.
+struct DenseRun {
+    uint32_t entry, split, nsplit, first, chunk, len;
+    // All of it is the same for the wavefront; loads that depend on it alone are scalar ones.
+    __device__ __forceinline__ void to_scalars()
+    {
+        entry = __builtin_amdgcn_readfirstlane(entry);
+        split = __builtin_amdgcn_readfirstlane(split);
+        nsplit = __builtin_amdgcn_readfirstlane(nsplit);
+        first = __builtin_amdgcn_readfirstlane(first);
+        chunk = __builtin_amdgcn_readfirstlane(chunk);
+        len = __builtin_amdgcn_readfirstlane(len);
+    }
+};
+__device__ __forceinline__ uint32_t units_of(uint32_t len) { return (len + kDenseUnit - 1) / kDenseUnit; }
+// Sequence lengths, 64 at a time; the first 64 stay in a register.
+struct Lengths {
+    const DenseShares& s;
+    uint32_t most, lane, first;
+    __device__ __forceinline__ Lengths(const DenseShares& shares, uint32_t n_tokens) : s(shares), most(n_tokens), lane(threadIdx.x & 63), first(load(0)) {}
+    __device__ __forceinline__ uint32_t load(uint32_t o) const
+    {
+        return o + lane < s.batch ? static_cast<uint32_t>(min(max(s.lens[o + lane], 0), static_cast<int32_t>(most))) : 0;
+    }
+    __device__ __forceinline__ uint32_t at(uint32_t o) const { return o ? load(o) : first; }
+    // Runs of `chunk` units (inv: about its inverse).  Units are below 2^24, so that a binary32 quotient is off by one at most.  An
+    // empty sequence has a run too: it writes zeros.
+    __device__ __forceinline__ uint32_t runs(uint32_t o, uint32_t len, uint32_t chunk, float inv) const
+    {
+        const uint32_t u = units_of(len) + chunk - 1;
+        uint32_t n = static_cast<uint32_t>(static_cast<float>(u) * inv);
+        const int32_t left = static_cast<int32_t>(u - n * chunk);
+        n += left < 0 ? -1 : left >= static_cast<int32_t>(chunk) ? 1 : 0;
+        return o + lane < s.batch ? max(n, 1u) : 0;
+    }
+};
+// Uniform over the wavefront.  entry == batch: there is no such run.
+__device__ __forceinline__ DenseRun find_run(const DenseShares& s, uint32_t number, int64_t n_tokens)
+{
+    DenseRun r;
+    if (!s.lens) {
+        r.entry = s.by_nsplit.over(number);
+        r.nsplit = s.nsplit;
+        r.first = r.entry * s.nsplit;
+        r.split = number - r.first;
+        r.chunk = s.chunk;
+        r.len = static_cast<uint32_t>(n_tokens);
+        return r;
+    }
+    const Lengths lens(s, static_cast<uint32_t>(n_tokens));
+    r.chunk = s.units;
+    if (s.most_runs) {
+        uint32_t total = 0;
+        for (uint32_t o = 0; o < s.batch; o += 64) total += units_of(lens.at(o));
+        total = wave_sum(total);
+        // Each sequence rounds up to whole runs, so that total / most_runs may be too small.  With total / (most_runs -
+        // batch) there are never too many.
+        const uint32_t safe = s.by_spare.over(total + s.by_spare.d - 1);
+        uint32_t chunk = max(s.by_most.over(total + s.most_runs - 1), 1u);
+        for (int tries = 0; chunk < safe; ++tries) {
+            uint32_t made = 0;
+            const float inv = __builtin_amdgcn_rcpf(static_cast<float>(chunk));
+            for (uint32_t o = 0; o < s.batch; o += 64) made += lens.runs(o, lens.at(o), chunk, inv);
+            made = wave_sum(made);
+            if (made <= s.most_runs) break;
+            chunk = tries < 3 ? max(chunk + 1, s.by_most.over(chunk * made)) : safe;
+        }
+        r.chunk = min(max(chunk, 1u), s.units);
+    }
+    r.entry = s.batch;
+    r.nsplit = r.first = r.split = 0;
+    r.len = 0;
+    const float inv = __builtin_amdgcn_rcpf(static_cast<float>(r.chunk));
+    for (uint32_t o = 0, before = 0; o < s.batch; o += 64) {
+        const uint32_t len = lens.at(o), n = lens.runs(o, len, r.chunk, inv);
+        const uint32_t upto = before + wave_inclusive_scan(n);
+        const unsigned long long past = __ballot(upto > number);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            r.entry = o + at;
+            r.nsplit = __builtin_amdgcn_readlane(n, at);
+            r.first = __builtin_amdgcn_readlane(upto, at) - r.nsplit;
+            r.split = number - r.first;
+            r.len = __builtin_amdgcn_readlane(len, at);
+            break;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    return r;
+}
+
 // A running softmax sum of partial results.
 struct Join {
     float m = -INFINITY, l = 0.0f;
@@ -172,11 +284,12 @@ struct Join {
     }
 };
 
-// Joins the partial results of rows row0 .. row0 + rows - 1 into out, in the workgroup that arrived last.  A group of 64
-// threads has a row, two columns a thread, and NB splits on their way at once; where there are fewer rows than groups,
-// the groups share out each row's splits and are joined in order.  `lds`: 128 f32x2 for each group but the first.
+// Joins the partial results of `rows` rows into out, in the workgroup that arrived last: those of row r are the nsplit ones
+// at + r, at + r + step, ...  A group of 64 threads has a row, two columns a thread, and NB splits on their way
+// at once; where there are fewer rows than groups, the groups share out each row's splits and are joined in order.  `lds`: 128
+// f32x2 for each group but the first.
 template <int NT, uint32_t NB>
-__device__ __forceinline__ void join_rows(const Partials& p, uint32_t row0, uint32_t rows, uint32_t nsplit, float* out, f32x2* lds)
+__device__ __forceinline__ void join_rows(const Partials& p, uint32_t at, uint32_t step, uint32_t rows, uint32_t nsplit, float* out, f32x2* lds)
 {
     constexpr uint32_t GROUPS = NT / 64;
     const uint32_t c = threadIdx.x & 63, group = threadIdx.x >> 6;
@@ -189,9 +302,9 @@ __device__ __forceinline__ void join_rows(const Partials& p, uint32_t row0, uint
             f32x2 ml[NB], v[NB];
 #pragma unroll
             for (uint32_t y = 0; y < NB; ++y) {
-                const size_t at = static_cast<size_t>(row0 + r) * nsplit + min(s + stride * y, nsplit - 1);
-                ml[y] = get_pair(p.ml + at);
-                v[y] = get_pair(p.acc + at * 64 + c);
+                const size_t from = at + r + static_cast<size_t>(min(s + stride * y, nsplit - 1)) * step;
+                ml[y] = get_pair(p.ml + from);
+                v[y] = get_pair(p.acc + from * 64 + c);
             }
 #pragma unroll
             for (uint32_t y = 0; y < NB; ++y)
@@ -209,11 +322,15 @@ __device__ __forceinline__ void join_rows(const Partials& p, uint32_t row0, uint
 #pragma unroll
             for (uint32_t k = 0; k + 1 < GROUPS; ++k) j.add(lds[k * 128 + c], lds[k * 128 + 64 + c]);
         }
-        o[static_cast<size_t>(row0 + r) * 64 + c] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
+        o[static_cast<size_t>(r) * 64 + c] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
     }
 }
 
 #endif   // __HIPCC__
 
 }  // namespace cache
+
+// Joins partial results; `about`: splits of a row, on average.
+int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const void* part_acc, const cache::MergeRows& r, int64_t about, float* out);
+
 }  // namespace spotlight

@@ -224,7 +224,7 @@ __global__ __launch_bounds__(NT) void cache_attend_kernel(AttendArgs a)
     if constexpr (JOINS) {
         if (!a.part.arrived) return;
         if (arrives_last(a.part.arrived + bh * kArrivedStride, static_cast<uint32_t>(a.nsplit), &s_before))
-            join_rows<NT, 16>(a.part, static_cast<uint32_t>(bh), 1, static_cast<uint32_t>(a.nsplit), a.out, reinterpret_cast<f32x2*>(&s_acc[0][0]));
+            join_rows<NT, 16>(a.part, static_cast<uint32_t>(bh) * a.nsplit, 1, 1, static_cast<uint32_t>(a.nsplit), a.out + bh * kHeadDim, reinterpret_cast<f32x2*>(&s_acc[0][0]));
     }
 }
 
@@ -233,7 +233,7 @@ void launch_rb(spotlight_ctx* ctx, StageTimer& timer, AttendArgs& a)
 {
     const Plan& p = ctx->plan;
     a.nsplit = (a.topk + RB - 1) / RB;
-    if (NT == kWholeThreads || RB != kAttendMinRows || !joins_in_place(static_cast<int64_t>(p.B) * p.Hq, 1, a.nsplit)) a.part.arrived = nullptr;
+    if (NT == kWholeThreads || RB != kAttendMinRows || !joins_in_place(static_cast<int64_t>(p.B) * p.Hq * a.nsplit, 1, a.nsplit)) a.part.arrived = nullptr;
     if (timer.rec) timer.rec->whole = NT == kWholeThreads || a.part.arrived;
     timer.launch(cache_attend_kernel<CT, QT, RB, NT>, dim3(static_cast<unsigned>(a.nsplit), static_cast<unsigned>(p.B * p.Hq)), dim3(NT), 0, a);
 }
@@ -253,7 +253,7 @@ int launch_t(spotlight_ctx* ctx, AttendArgs& a)
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
     if (a.nsplit == 1 || a.part.arrived) return SPOTLIGHT_OK;
-    return launch_cache_merge(ctx, a.part.ml, a.part.acc, heads, a.nsplit, a.out);
+    return launch_cache_merge(ctx, a.part.ml, a.part.acc, MergeRows{heads, a.nsplit, nullptr, {}, {}, {}, 0, 0}, a.nsplit, a.out);
 }
 
 }  // namespace

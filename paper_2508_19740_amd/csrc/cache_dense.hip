@@ -122,15 +122,14 @@ struct DenseArgs {
     const uint8_t* v;
     const float* k_scale;
     const float* v_scale;
-    const int32_t* lens;
     Partials part;
+    uint2* runs;                        // [batch] {first, number} of each sequence's runs, for the merge
     float* out;
     int64_t Nmax, blocks, n_tokens;
-    int64_t chunk;                      // keys of a split, a multiple of kStep * kWaves
+    DenseShares shares;
+    FastDiv by_queries;
     uint32_t rows, n_q;                 // rows of a key-value head: G * n_q
-    uint32_t nsplit;
-    uint32_t turn;                      // by how much the splits of one head are turned against the last one's
-    int Hkv, shift;
+    int shift;
     float scale2;                       // |scale| * log2(e)
     bool negate;                        // the scale is negative: q is negated
 };
@@ -217,11 +216,19 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g = lane >> 4, i = lane & 15;
-    const uint32_t split = (blockIdx.x + a.turn * blockIdx.y) % a.nsplit, r0 = blockIdx.x / a.nsplit * (16 * MT);
-    const int64_t head = blockIdx.y;
-
-    int64_t len = a.n_tokens;
-    if (a.lens) len = min(max(static_cast<int64_t>(a.lens[blockIdx.y / static_cast<uint32_t>(a.Hkv)]), static_cast<int64_t>(0)), len);
+    // Workgroups go to the eight dies in turn: the tiles of one run and head, which read the same keys, to one die.
+    uint32_t group = blockIdx.x, tile = 0;
+    if (a.shares.tiles > 1) {
+        const uint32_t eighth = a.shares.by_tiles8.over(blockIdx.x), in = blockIdx.x - eighth * a.shares.by_tiles8.d;
+        group = eighth * 8 + in % 8;
+        tile = in / 8;
+    }
+    const uint32_t number = a.shares.by_heads.over(group), heads = a.shares.by_heads.d, kv = group - number * heads;
+    DenseRun run = find_run(a.shares, number, a.n_tokens);
+    run.to_scalars();
+    if (run.entry >= a.shares.batch) return;
+    const uint32_t r0 = tile * (16 * MT), nsplit = run.nsplit;
+    const int64_t head = static_cast<int64_t>(run.entry) * heads + kv, len = run.len;
 
     // The queries of the tile's rows: first of them, last of them, and those of the lane's rows.  Rows behind the
     // last repeat it.
@@ -230,18 +237,18 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     for (int t = 0; t < MT; ++t) { row[t] = min(r0 + 16 * t + i, a.rows - 1); query[t] = 0; }
     if (a.n_q > 1) {
         const uint32_t last = min(r0 + 16 * MT, a.rows) - 1;
-        q_least = r0 % a.n_q;
-        q_most = last % a.n_q;
+        q_least = r0 - a.by_queries.over(r0) * a.n_q;
+        q_most = last - a.by_queries.over(last) * a.n_q;
         if (last - r0 >= a.n_q || q_least > q_most) { q_least = 0; q_most = a.n_q - 1; }
 #pragma unroll
-        for (int t = 0; t < MT; ++t) query[t] = row[t] % a.n_q;
+        for (int t = 0; t < MT; ++t) query[t] = row[t] - a.by_queries.over(row[t]) * a.n_q;
     }
     const int64_t before = len - a.n_q + 1;      // query x sees the keys before this + x
 
     // this wavefront's keys
-    const int64_t c0 = split * a.chunk, c1 = min(c0 + a.chunk, before + q_most);
-    const int64_t share = a.chunk / kWaves;
-    const int64_t k0 = c0 + wave * share;
+    const int64_t c0 = static_cast<int64_t>(run.split) * run.chunk * kDenseUnit;
+    const int64_t c1 = min(c0 + static_cast<int64_t>(run.chunk) * kDenseUnit, before + q_most);
+    const int64_t share = (max(c1 - c0, static_cast<int64_t>(0)) + kDenseUnit - 1) / kDenseUnit * kStep, k0 = c0 + wave * share;
     const int n = static_cast<int>(min(max(c1 - k0, static_cast<int64_t>(0)), share));
     const int steps = (n + kStep - 1) / kStep;
     // the first steps, whose keys every row sees
@@ -470,34 +477,89 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             Join j;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) j.add(f32x2{s_m[w][row], s_l[w][row]}, reinterpret_cast<const f32x2*>(s_acc[w][row])[pair]);
-            const size_t at = head * a.rows + r0 + 16 * t + row;
-            if (a.nsplit == 1) {
-                reinterpret_cast<f32x2*>(a.out + at * kHeadDim)[pair] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
-            } else {
-                put_part(a.part, at * a.nsplit + split, pair, j.m, j.l, j.a);
-            }
+            if (nsplit == 1)
+                reinterpret_cast<f32x2*>(a.out + (head * a.rows + r0 + 16 * t + row) * kHeadDim)[pair] = j.l != 0.0f ? f32x2{j.a.x / j.l, j.a.y / j.l} : f32x2{0.0f, 0.0f};
+            else
+                put_part(a.part, static_cast<size_t>(group * a.shares.tiles + tile) * a.shares.tile_rows + 16 * t + row, pair, j.m, j.l, j.a);
         }
     }
-    if (a.nsplit == 1 || !a.part.arrived) return;
-    const uint32_t tiles = gridDim.x / a.nsplit;
-    if (arrives_last(a.part.arrived + (blockIdx.y * tiles + blockIdx.x / a.nsplit) * kArrivedStride, a.nsplit, &s_before))
-        join_rows<kThreads, 16>(a.part, static_cast<uint32_t>(head) * a.rows + r0, min(16u * MT, a.rows - r0), a.nsplit, a.out, reinterpret_cast<f32x2*>(&s_acc[0][0][0]));
+    // (No store may come before the scales have been read: they would not be scalar loads.)
+    if (kv == 0 && tile == 0 && run.split == 0 && tid == 0) a.runs[run.entry] = make_uint2(run.first, nsplit);
+    if (nsplit == 1 || !a.part.arrived) return;
+    const uint32_t first = (run.first * heads + kv) * a.shares.tiles + tile;          // the same tile in the sequence's first run
+    if (arrives_last(a.part.arrived + first * kArrivedStride, nsplit, &s_before))
+        join_rows<kThreads, 16>(a.part, first * a.shares.tile_rows, heads * a.shares.tiles * a.shares.tile_rows, min(16u * MT, a.rows - r0), nsplit,
+                                a.out + (head * a.rows + r0) * kHeadDim, reinterpret_cast<f32x2*>(&s_acc[0][0][0]));
 }
 
 template <typename CT, typename QT>
-void launch_mt(spotlight_ctx* ctx, StageTimer& timer, DenseArgs& a, int mt)
+void launch_mt(StageTimer& timer, const DenseArgs& a, const DensePlan& d)
 {
-    const Plan& p = ctx->plan;
-    const dim3 grid((a.rows + 16 * mt - 1) / (16 * mt) * a.nsplit, static_cast<unsigned>(p.B * p.Hkv));
-    // Workgroups go to the eight dies in turn.  Sequences of different lengths use their first splits most, so split s of
-    // head y belongs on die s + y, whatever the width of the grid: with 16 splits of 16 sequences of 2049 .. 32769
-    // tokens all dies work as long (81 -> 67 us).
-    a.turn = grid.x % 8 + 7;
-    auto kern = mt == 1 ? cache_dense_kernel<CT, QT, 1> : cache_dense_kernel<CT, QT, 2>;
-    timer.launch(kern, grid, dim3(kThreads), 0, a);
+    auto kern = d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1> : cache_dense_kernel<CT, QT, 2>;
+    timer.launch(kern, dim3(d.grid), dim3(kThreads), 0, a);
 }
 
 }  // namespace
+
+namespace cache {
+int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d)
+{
+    const int64_t rows = static_cast<int64_t>(p.G) * n_q;
+    if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;
+    DenseShares& s = d->shares;
+    d->row_tiles = rows <= 16 ? 1 : 2;
+    const int64_t most_rows = 16 * d->row_tiles, tiles = (rows + most_rows - 1) / most_rows, per = tiles * p.Hkv;   // workgroups of a run
+    s.lens = lens;
+    s.batch = static_cast<uint32_t>(p.B);
+    s.tiles = static_cast<uint32_t>(tiles);
+    s.tile_rows = static_cast<uint32_t>(rows < most_rows ? rows : most_rows);
+    const int64_t units = (n_tokens + kDenseUnit - 1) / kDenseUnit, B = p.B;
+    // Runs of all sequences: two workgroups a compute unit, which it holds at once (of the kernel with 16 rows it would hold
+    // three; those measured the same or slower, 62 against 64 us for 16 sequences of different lengths), as far as there is
+    // room for their partial results.
+    const int64_t hold = static_cast<int64_t>(n_cus) * 2 / per, room = p.dense_rows / (s.tile_rows * per);
+    int64_t runs, most, chunk;
+    s.most_runs = 0;
+    if (!lens) {
+        most = std::min({hold / B, room / B, units});
+        const int64_t need = (n_tokens + kDenseMostKeys - 1) / kDenseMostKeys;
+        if (most < need) {
+            most = need;
+            if (need > 1 && need > room / B) return SPOTLIGHT_ERR_UNSUPPORTED;
+        }
+        chunk = (units + most - 1) / most;
+        most = (units + chunk - 1) / chunk;
+        runs = B * most;
+    } else {
+        runs = std::min({std::max(hold, 2 * B), room, B * units});
+        if (units > 1 && runs > B) {
+            s.most_runs = static_cast<uint32_t>(runs);
+            chunk = std::min((B * units + runs - B - 1) / (runs - B), units);
+            most = std::min(units, runs - B + 1);
+        } else {
+            runs = B;
+            chunk = units;
+            most = 1;
+        }
+    }
+    if (chunk * kDenseUnit > kDenseMostKeys + kDenseUnit) return SPOTLIGHT_ERR_UNSUPPORTED;
+    const int64_t grid = (runs * p.Hkv + 7) / 8 * 8 * tiles;
+    if (grid > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;
+    s.units = static_cast<uint32_t>(units);
+    s.chunk = static_cast<uint32_t>(chunk);
+    s.nsplit = static_cast<uint32_t>(most);
+    s.by_nsplit = fast_div(s.nsplit);
+    s.by_most = fast_div(s.most_runs ? s.most_runs : 1);
+    s.by_spare = fast_div(s.most_runs ? s.most_runs - s.batch : 1);
+    s.by_heads = fast_div(static_cast<uint32_t>(p.Hkv));
+    s.by_tiles8 = fast_div(8 * s.tiles);
+    d->grid = static_cast<uint32_t>(tiles == 1 ? runs * p.Hkv : grid);
+    d->splits = most > 1;
+    d->about = runs / B;
+    d->joins = joins_in_place(runs * per, s.tile_rows, most);
+    return SPOTLIGHT_OK;
+}
+}  // namespace cache
 
 int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, int64_t n_tokens, int n_q, const int32_t* lens,
                        float scale, float* out)
@@ -509,7 +571,6 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     a.v = static_cast<const uint8_t*>(c.v);
     a.k_scale = c.k_scale;
     a.v_scale = c.v_scale;
-    a.lens = lens;
     a.part.ml = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_dense_ml);
     a.part.acc = reinterpret_cast<unsigned long long*>(ctx->workspace + p.off_dense_acc);
     a.out = out;
@@ -518,33 +579,34 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     a.n_tokens = n_tokens;
     a.rows = static_cast<uint32_t>(p.G) * static_cast<uint32_t>(n_q);
     a.n_q = static_cast<uint32_t>(n_q);
-    a.Hkv = p.Hkv;
     a.shift = __builtin_ctz(static_cast<unsigned>(c.block_tokens));
     a.scale2 = fabsf(scale) * kLog2e;
     a.negate = scale < 0.0f;
 
-    DenseSplit sp;
-    const int rc = split_dense(p, ctx->n_cus, n_tokens, n_q, &sp);
+    DensePlan d;
+    const int rc = plan_dense(p, ctx->n_cus, n_tokens, n_q, lens, &d);
     if (rc != SPOTLIGHT_OK) return rc;
-    a.chunk = sp.chunk;
-    a.nsplit = static_cast<uint32_t>(sp.nsplit);
-    const int64_t groups = static_cast<int64_t>(p.B) * p.Hkv * ((a.rows + 16 * sp.tiles - 1) / (16 * sp.tiles));
-    a.part.arrived = joins_in_place(groups, std::min<int64_t>(a.rows, 16 * sp.tiles), sp.nsplit) ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_arrived) : nullptr;
-    const bool done = sp.nsplit == 1 || a.part.arrived;       // nothing is left to merge
+    a.shares = d.shares;
+    a.by_queries = fast_div(a.n_q);
+    a.runs = reinterpret_cast<uint2*>(ctx->workspace + p.off_runs);
+    a.part.arrived = d.joins ? reinterpret_cast<uint32_t*>(ctx->workspace + p.off_arrived) : nullptr;
+    const bool done = !d.splits || d.joins;                   // nothing is left to merge
     {
         StageTimer timer(ctx, SPOTLIGHT_STAGE_ATTEND);
         if (timer.rec) timer.rec->whole = done;
         if (p.kv_dtype == SPOTLIGHT_BF16) {
-            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, bf16_raw>(ctx, timer, a, sp.tiles);
-            else launch_mt<I8, bf16_raw>(ctx, timer, a, sp.tiles);
+            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, bf16_raw>(timer, a, d);
+            else launch_mt<I8, bf16_raw>(timer, a, d);
         } else {
-            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, float>(ctx, timer, a, sp.tiles);
-            else launch_mt<I8, float>(ctx, timer, a, sp.tiles);
+            if (c.code_type == SPOTLIGHT_E4M3) launch_mt<E4M3, float>(timer, a, d);
+            else launch_mt<I8, float>(timer, a, d);
         }
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
     if (done) return SPOTLIGHT_OK;
-    return launch_cache_merge(ctx, a.part.ml, a.part.acc, static_cast<int64_t>(p.B) * p.Hkv * a.rows, sp.nsplit, out);
+    const MergeRows r{static_cast<int64_t>(p.B) * p.Hkv * a.rows, 0, a.runs, fast_div(a.rows), fast_div(static_cast<uint32_t>(p.Hkv)),
+                      fast_div(16u * d.row_tiles), d.shares.tiles, d.shares.tile_rows};
+    return launch_cache_merge(ctx, a.part.ml, a.part.acc, r, d.about, out);
 }
 
 }  // namespace spotlight

@@ -10,7 +10,7 @@ namespace {
 // out: its accumulator may hold anything.
 template <int PARTS>
 __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __restrict__ part_ml, const float4* __restrict__ part_acc,
-                                                               float4* __restrict__ out, int64_t rows, int nsplit)
+                                                               float4* __restrict__ out, MergeRows r)
 {
     constexpr int NB = 8, QUADS = kHeadDim / 4, RPW = kThreads / QUADS / PARTS;   // rows of a workgroup
     __shared__ float s_m[PARTS][kThreads / PARTS], s_l[PARTS][kThreads / PARTS];
@@ -18,7 +18,18 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __r
     const int tid = threadIdx.x;
     const int c = tid % QUADS, part = tid / QUADS % PARTS, slot = tid / (QUADS * PARTS);
     const int64_t row = static_cast<int64_t>(blockIdx.x) * RPW + slot;
-    const int64_t at = min(row, rows - 1) * nsplit;       // threads behind the last row repeat it
+    const int64_t have = min(row, r.rows - 1);            // threads behind the last row repeat it
+    int64_t at = have * r.nsplit, step = 1;
+    int nsplit = r.nsplit;
+    if (r.runs) {
+        const uint32_t head = r.by_rows.over(static_cast<uint32_t>(have)), in_head = static_cast<uint32_t>(have) - head * r.by_rows.d;
+        const uint32_t entry = r.by_heads.over(head), tile = r.by_tile.over(in_head);
+        const uint2 run = r.runs[entry];
+        nsplit = static_cast<int>(run.y);
+        at = (static_cast<int64_t>(run.x) * r.by_heads.d + (head - entry * r.by_heads.d)) * r.tiles + tile;
+        at = at * r.tile_rows + (in_head - tile * r.by_tile.d);
+        step = static_cast<int64_t>(r.by_heads.d) * r.tiles * r.tile_rows;
+    }
     float m = -INFINITY, l = 0.0f;
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int s0 = part; s0 < nsplit; s0 += PARTS * NB) {
@@ -27,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __r
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             const int sp = s0 + PARTS * i;
-            const int64_t spc = at + (sp < nsplit ? sp : s0);      // in-bounds stand-in, left out below
+            const int64_t spc = at + (sp < nsplit ? sp : s0) * step;      // in-bounds stand-in, left out below
             v[i] = part_ml[spc];
             av[i] = part_acc[spc * QUADS + c];
             if (sp >= nsplit) v[i].y = 0.0f;
@@ -69,20 +80,20 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __r
             }
         }
     }
-    if (row >= rows) return;
+    if (row >= r.rows || (r.runs && nsplit == 1)) return;      // a sequence of one run has its result already
     out[row * QUADS + c] = l != 0.0f ? make_float4(a.x / l, a.y / l, a.z / l, a.w / l) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 }
 
 }  // namespace
 
-int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const void* part_acc, int64_t rows, int nsplit, float* out)
+int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const void* part_acc, const MergeRows& r, int64_t about, float* out)
 {
     StageTimer timer(ctx, SPOTLIGHT_STAGE_MERGE);
     // few splits: a row's are folded by the same threads, and a workgroup has eight rows
-    const bool few = nsplit <= 8;
+    const bool few = about <= 8;
     const int64_t per = few ? kThreads / (kHeadDim / 4) : 1;
-    timer.launch(few ? cache_merge_kernel<1> : cache_merge_kernel<8>, dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kThreads), 0,
-                 static_cast<const float2*>(part_ml), static_cast<const float4*>(part_acc), reinterpret_cast<float4*>(out), rows, nsplit);
+    timer.launch(few ? cache_merge_kernel<1> : cache_merge_kernel<8>, dim3(static_cast<unsigned>((r.rows + per - 1) / per)), dim3(kThreads), 0,
+                 static_cast<const float2*>(part_ml), static_cast<const float4*>(part_acc), reinterpret_cast<float4*>(out), r);
     return hip_rc(hipGetLastError());
 }
 

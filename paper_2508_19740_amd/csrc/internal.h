@@ -50,6 +50,7 @@ struct Plan {
     size_t off_dense_ml;   // [dense_rows] {max, sum} of each split of attention over the whole 8-bit cache
     size_t off_dense_acc;  // [dense_rows][128] weighted value sums of each split
     int64_t dense_rows;
+    size_t off_runs;       // [B] {first run, runs} of each sequence in that attention
     size_t off_arrived;    // [kArrivedBytes] workgroups of each group of rows that have written their part; 0 between calls
     size_t off_audit;      // AuditRec of the bulk hash (SPOTLIGHT_OPT_BULK_HASH_AUDIT)
     size_t total_bytes;
@@ -203,9 +204,6 @@ int launch_cache_read(spotlight_ctx* ctx, const spotlight_cache& c, int64_t t0, 
 int launch_cache_attend(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, const int32_t* idx, int k, float scale, float* out);
 int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache& c, int64_t n_tokens, int n_q, const int32_t* lens,
                        float scale, float* out);
-
-// Joins the nsplit partial results {max in units of log2, sum} and weighted sums of values of each row.
-int launch_cache_merge(spotlight_ctx* ctx, const void* part_ml, const void* part_acc, int64_t rows, int nsplit, float* out);
 
 // Error bound of the matrix-core last hash layer per unit of ||W2[j]|| * ||h||, n terms long (hash_bulk.h): the rounding of
 // partial sums, which are at most as large as the terms before them or as the result and the terms behind them,

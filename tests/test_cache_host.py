@@ -15,6 +15,7 @@ CSRC = os.path.join(ROOT, "paper_2508_19740_amd", "csrc")
 HEAD = r"""
 #include <stdio.h>
 #include <string.h>
+#include <algorithm>
 #include "cache.h"
 using namespace spotlight;
 static spotlight_config config(int B, int Hq, int Hkv, long n, int k)
@@ -102,8 +103,12 @@ int main()
     // a long cache whose many rows leave no room for the splits it needs
     const spotlight_config lc = config(1, 1, 1, 1L << 27, 50);
     if (make_plan(&lc, &ctx.plan) != SPOTLIGHT_OK) return 2;
-    cache::DenseSplit s;
-    WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::split_dense(ctx.plan, 256, 1L << 27, 16384, &s));
+    cache::DensePlan d;
+    WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::plan_dense(ctx.plan, 256, 1L << 27, 16384, nullptr, &d));
+    WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::plan_dense(ctx.plan, 256, 1L << 27, 16384, i, &d));
+    WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::plan_dense(ctx.plan, 256, 100, (1 << 24) + 1, nullptr, &d));
+    WANT(SPOTLIGHT_OK, cache::plan_dense(ctx.plan, 256, 1L << 27, 1, nullptr, &d));
+    WANT(SPOTLIGHT_OK, cache::plan_dense(ctx.plan, 256, 1L << 27, 1, i, &d));
     return failed;
 }
 """
@@ -122,17 +127,57 @@ int main()
                     for (long n : {1L, cap / 3 + 1, cap})
                         for (long nq : {1L, 2L, 5L, 17L, 128L, 1000L, cap}) {
                             if (nq > cap || nq > 2147483647L) continue;
-                            cache::DenseSplit s;
-                            const int rc = cache::split_dense(p, 256, n, static_cast<int>(nq), &s);
-                            const long all = static_cast<long>(B) * Hkv * G * nq;
-                            if (rc == SPOTLIGHT_ERR_UNSUPPORTED && (n > cache::kDenseMostKeys || G * nq > 1 << 24)) continue;
-                            const bool ok = rc == SPOTLIGHT_OK && (s.tiles == 1 || s.tiles == 2 || s.tiles == 4) && s.nsplit >= 1 &&
-                                s.chunk % (cache::kDenseStep * cache::kDenseWaves) == 0 && s.chunk <= cache::kDenseMostKeys + 127 &&
-                                s.chunk * s.nsplit >= n && s.chunk * (s.nsplit - 1) < n && (s.nsplit == 1 || all * s.nsplit <= p.dense_rows);
-                            if (!ok) {
-                                printf("B %d Hkv %d G %d cap %ld n %ld nq %ld: rc %d tiles %d nsplit %d chunk %ld\n", B, Hkv, G, cap, n, nq, rc,
-                                       s.tiles, s.nsplit, static_cast<long>(s.chunk));
-                                return 1;
+                            for (int ragged : {0, 1}) {
+                                cache::DensePlan d;
+                                int32_t one;
+                                const int rc = cache::plan_dense(p, 256, n, static_cast<int>(nq), ragged ? &one : nullptr, &d);
+                                const cache::DenseShares& s = d.shares;
+                                const long rows = static_cast<long>(G) * nq, units = (n + 127) / 128;
+                                if (rc == SPOTLIGHT_ERR_UNSUPPORTED && (n > 1 << 24 || rows > 1 << 24 || B * Hkv * rows / 32 > 1 << 23)) continue;
+                                bool ok = rc == SPOTLIGHT_OK && (d.row_tiles == 1 || d.row_tiles == 2) && s.tile_rows * s.tiles >= rows &&
+                                    s.tile_rows <= 16 * d.row_tiles && s.chunk * 128L <= (1L << 25) + 128 && d.grid <= 1 << 24;
+                                long runs = 0;
+                                if (!ragged) {
+                                    runs = static_cast<long>(B) * s.nsplit;
+                                    ok = ok && s.nsplit >= 1 && static_cast<long>(s.chunk) * s.nsplit >= units && static_cast<long>(s.chunk) * (s.nsplit - 1) < units;
+                                } else {
+                                    // lengths all alike, all short but one, none at all: the runs they make fit the grid and the workspace
+                                    for (int kind = 0; kind < 3; ++kind) {
+                                        long total = 0, made = 0;
+                                        for (int b = 0; b < B; ++b) total += kind == 0 ? units : kind == 1 && b == B / 2 ? units : 0;
+                                        long chunk = units;                  // as the kernel chooses it
+                                        if (s.most_runs) {
+                                            const long safe = (total + s.most_runs - B - 1) / (s.most_runs - B);
+                                            chunk = std::max((total + s.most_runs - 1) / s.most_runs, 1L);
+                                            for (int tries = 0; chunk < safe; ++tries) {
+                                                long m = 0;
+                                                for (int b = 0; b < B; ++b)
+                                                    m += std::max(((kind == 0 ? units : kind == 1 && b == B / 2 ? units : 0) + chunk - 1) / chunk, 1L);
+                                                if (m <= s.most_runs) break;
+                                                chunk = tries < 3 ? std::max(chunk + 1, chunk * m / s.most_runs) : safe;
+                                            }
+                                            chunk = std::min(std::max(chunk, 1L), units);
+                                        }
+                                        ok = ok && chunk * 128 <= (1L << 25) + 128;
+                                        for (int b = 0; b < B; ++b) {
+                                            const long u = kind == 0 ? units : kind == 1 && b == B / 2 ? units : 0, r = std::max((u + chunk - 1) / chunk, 1L);
+                                            ok = ok && r <= s.nsplit;
+                                            made += r;
+                                        }
+                                        runs = std::max(runs, made);
+                                    }
+                                }
+                                ok = ok && (s.tiles == 1 ? runs * Hkv <= d.grid : (runs * Hkv + 7) / 8 * 8 * s.tiles <= d.grid);
+                                ok = ok && d.splits == (s.nsplit > 1) && (!d.splits || runs * Hkv * s.tiles * s.tile_rows <= p.dense_rows);
+                                ok = ok && (!d.joins || runs * Hkv * s.tiles <= kJoinGroups);
+                                for (const cache::FastDiv& f : {s.by_nsplit, s.by_heads, s.by_tiles8, s.by_most, s.by_spare})
+                                    for (uint32_t x : {0u, 1u, f.d - 1, f.d, f.d + 1, 5 * f.d - 1, 5 * f.d, 99999u, (1u << 24) + 1, (1u << 31) - 1})
+                                        if (x < 1u << 31) ok = ok && x / f.d == static_cast<uint32_t>((static_cast<uint64_t>(x) * f.mul >> 32) + x) >> f.shift;
+                                if (!ok) {
+                                    printf("B %d Hkv %d G %d cap %ld n %ld nq %ld ragged %d: rc %d tiles %u nsplit %u chunk %u most %u runs %ld\n", B, Hkv, G, cap, n, nq,
+                                           ragged, rc, s.tiles, s.nsplit, s.chunk, s.most_runs, runs);
+                                    return 1;
+                                }
                             }
                         }
                 }

@@ -111,6 +111,11 @@ DENSE = [  # b, hq, hkv, n, n_q, block, code, kv, lens
     (2, 8, 1, 2500, 1, 64, "i8", "bf16", [-4, 9000]),                          # lengths out of range: taken into it
     (16, 8, 2, 300, 3, 32, "e4m3", "bf16", list(range(0, 320, 20))),
     (1, 2, 1, 20011, 1, 64, "e4m3", "bf16", None),
+    # many sequences of lengths of their own: one long among short ones, more than a wavefront has lanes, several tiles of rows
+    (130, 2, 1, 900, 1, 32, "e4m3", "bf16", [900 if b == 77 else 13 * b % 140 for b in range(130)]),
+    (70, 4, 2, 260, 20, 16, "i8", "bf16", [(37 * b) % 261 for b in range(70)]),
+    (3, 2, 2, 12000, 2, 128, "i8", "f32", [12000, 5, 700]),
+    (600, 1, 1, 130, 1, 16, "i8", "bf16", [b % 131 for b in range(600)]),
 ]
 
 
