@@ -129,6 +129,7 @@ class Cache:
                 raise ValueError(f"{name}: want contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
         self._args = CacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _CODE_TYPES[k.dtype], block_tokens)
+        self._ref = C.byref(self._args)
 
 
 def _dtype_code(t: torch.dtype) -> int:
@@ -182,6 +183,7 @@ class Spotlight:
         self._h = h
         # what every call compares its tensors with
         self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._scale = 1.0 / math.sqrt(head_dim)
         self._q_shape, self._out_shape = (batch, n_q_heads, head_dim), (batch, n_q_heads, head_dim)
         self._kv_shape, self._codes_shape = (batch, n_kv_heads, max_tokens, head_dim), (batch, n_kv_heads, max_tokens, self.W)
         if hidden > 0:
@@ -340,7 +342,7 @@ class Spotlight:
             raise TypeError("cache: want a Cache")
         if cache.k.shape != self._kv_shape or cache.k.device != self.device:
             raise ValueError(f"cache: want {self._kv_shape} on {self.device}, got {tuple(cache.k.shape)} on {cache.k.device}")
-        return C.byref(cache._args)
+        return cache._ref
 
     def _per_entry(self, t, name):
         return None if t is None else self._chk(t, (self.B,), torch.int32, name)
@@ -363,15 +365,26 @@ class Spotlight:
         """Rows t0 + first[b] .. + n - 1 of the cache as K, V [B, Hkv, n, d] in kv_dtype."""
         self._sync_stream()
         shape = (self.B, self.Hkv, n, self.d)
+        # what is made here needs no check; a second tensor like the first takes half the time of one from its shape
         if K is None:
-            K = torch.empty(shape, dtype=self.kv_dtype, device=self.device)
+            K = torch.empty(shape, dtype=self.kv_dtype, device=self.device) if V is None else torch.empty_like(V)
+        else:
+            self._chk(K, shape, self.kv_dtype, "K")
         if V is None:
-            V = torch.empty(shape, dtype=self.kv_dtype, device=self.device)
-        rc = lib.spotlight_cache_read(self._h, self._cache(cache), t0, n, self._per_entry(first, "first"),
-                                      self._chk(K, shape, self.kv_dtype, "K"), self._chk(V, shape, self.kv_dtype, "V"))
+            V = torch.empty_like(K)
+        else:
+            self._chk(V, shape, self.kv_dtype, "V")
+        rc = lib.spotlight_cache_read(self._h, self._cache(cache), t0, n, self._per_entry(first, "first"), K.data_ptr(), V.data_ptr())
         if rc != OK:
             raise SpotlightError(rc, "spotlight_cache_read")
         return K, V
+
+    def _result(self, q, out, shape):
+        """The float32 result of attention for q: `out`, checked, or a new tensor."""
+        if out is None:
+            return torch.empty_like(q, dtype=torch.float32)
+        self._chk(out, shape, torch.float32, "out")
+        return out
 
     def sparse_decode_cache(self, q, cache: Cache, idx, scale: Optional[float] = None, out=None):
         self._sync_stream()
@@ -380,12 +393,10 @@ class Spotlight:
             raise ValueError("idx: want [B, Hq, k]")
         k = idx.shape[-1]
         ip = self._chk(idx, (self.B, self.Hq, k), torch.int32, "idx")
-        if out is None:
-            out = torch.empty(self._out_shape, dtype=torch.float32, device=self.device)
-        op = self._chk(out, self._out_shape, torch.float32, "out")
+        out = self._result(q, out, self._out_shape)
         if scale is None:
-            scale = 1.0 / math.sqrt(self.d)
-        rc = lib.spotlight_sparse_decode_cache(self._h, qp, self._cache(cache), ip, k, float(scale), op)
+            scale = self._scale
+        rc = lib.spotlight_sparse_decode_cache(self._h, qp, self._cache(cache), ip, k, scale, out.data_ptr())
         if rc != OK:
             raise SpotlightError(rc, "spotlight_sparse_decode_cache")
         return out
@@ -397,13 +408,11 @@ class Spotlight:
         n_q = q.shape[2] if q.dim() == 4 else 1
         shape = (self.B, self.Hq, n_q, self.d) if q.dim() == 4 else self._q_shape
         qp = self._chk(q, shape, self.kv_dtype, "q")
-        if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=self.device)
-        op = self._chk(out, shape, torch.float32, "out")
+        out = self._result(q, out, shape)
         if scale is None:
-            scale = 1.0 / math.sqrt(self.d)
-        rc = lib.spotlight_dense_decode_cache(self._h, qp, self._cache(cache), n_tokens, n_q, self._per_entry(lens, "lens"),
-                                              float(scale), op)
+            scale = self._scale
+        rc = lib.spotlight_dense_decode_cache(self._h, qp, self._cache(cache), n_tokens, n_q, self._per_entry(lens, "lens"), scale,
+                                              out.data_ptr())
         if rc != OK:
             raise SpotlightError(rc, "spotlight_dense_decode_cache")
         return out

@@ -67,13 +67,20 @@ int make_plan(const spotlight_config* c, Plan* p)
     p->off_operands = off;  off = align_up(off + wheads * screen_operand_bytes(p->hidden, p->W), 256);
     p->off_open = off;      off = align_up(off + kheads * ((p->Nmax + 31) / 32) * 4, 256);
     p->off_open_counts = off; off = align_up(off + kheads * ((p->Nmax + 65535) / 65536) * 128, 256);
-    // Partial results of attention over the whole 8-bit cache: enough for 512 workgroups of 32 rows, or 1024 of 16, and
-    // for every query twice; fewer where the cache cannot be split that far.
+    // Partial results of attention over the whole 8-bit cache: enough for 512 workgroups of 32 rows, and
+    // for every query twice; fewer where the cache cannot be split that far.  A call of that attention leaves what
+    // retrieval keeps between its kernels unused, so that they lie there if there is room.
     const int64_t whole = static_cast<int64_t>(BH), least = 2 * whole, most = whole * ((p->Nmax + 127) / 128) * 8;
     p->dense_rows = most < 16384 ? most : 16384;
     if (p->dense_rows < least) p->dense_rows = least;
-    p->off_dense_ml = off;  off = align_up(off + static_cast<size_t>(p->dense_rows) * 8, 256);
-    p->off_dense_acc = off; off = align_up(off + static_cast<size_t>(p->dense_rows) * kHeadDim * 4, 256);
+    const size_t ml_bytes = align_up(static_cast<size_t>(p->dense_rows) * 8, 256), acc_bytes = static_cast<size_t>(p->dense_rows) * kHeadDim * 4;
+    if (p->off_wnorm - p->off_gcum >= ml_bytes + acc_bytes) {
+        p->off_dense_ml = p->off_gcum;
+    } else {
+        p->off_dense_ml = off;
+        off = align_up(off + ml_bytes + acc_bytes, 256);
+    }
+    p->off_dense_acc = p->off_dense_ml + ml_bytes;
     p->off_runs = off;      off = align_up(off + static_cast<size_t>(p->B) * 8, 256);
     p->off_arrived = off;   off = align_up(off + kArrivedBytes, 256);
     p->off_audit = off;     off = align_up(off + sizeof(AuditRec), 256);

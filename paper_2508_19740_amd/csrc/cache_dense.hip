@@ -8,9 +8,9 @@
 //                   bytes of key i; four products take 8 of them each, and q lies in registers in the
 //                   same order.  The result leaves lane (g, i) with keys 4g .. 4g+3 of query row i.
 //   softmax         weights are relative to a maximum that was taken once.  Lanes compare their own scores
-//                   with it, and only where one is more than 4 (a factor of 16) above it is the maximum taken
+//                   with it, and only where one is more than 8 (a factor of 2^8) above it is the maximum taken
 //                   anew, over the lanes, and what has been summed rescaled.  (Taken at every larger score, some row
-//                   of 16 had one at most steps.)
+//                   of 16 had one at most steps; at 4 above, at one step in three.)
 //   O^T += V^T P^T  The lane holds the weights just where the second operand wants them (the keys of a
 //                   product may come in any order).  The first operand wants the same keys of one
 //                   column: lane (g, i) loads 8 bytes, columns 8i .. 8i+7, of each of its eight keys, and
@@ -18,8 +18,9 @@
 //
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
-//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (20 bits).
-//   p   is in [0, 16], scaled by 2^11 and split in two parts: 20 bits, or 2^-35 where that is more.
+//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).
+//   p   is in [0, 2^8] (below), scaled by 2^7 and split in two parts: 22 bits, or 2^-32 of the largest weight
+//       where that is more.  Both are rounded to nearest: what many small weights lose must not add up.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
 //       ratio is above 2^-20, and at most 2^-30 of the largest block's size off below.
 //
@@ -40,11 +41,9 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = kDenseStep;       // keys of a step
-constexpr int kWaves = kDenseWaves;
-static_assert(kWaves == kThreads / 64, "wavefronts of a workgroup");
-constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^11
-constexpr float kPUp = 11.0f;
-constexpr float kSlack = 4.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
+constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^7
+constexpr float kPUp = 7.0f;
+constexpr float kSlack = 8.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
 constexpr int kInf = 0x7f800000;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -102,6 +101,9 @@ template <> struct Operand<I8> {
     }
 };
 
+// Two numbers rounded to binary16 (to nearest: what many small weights lose must not add up).
+__device__ __forceinline__ h2 to_half(float x, float y) { return __builtin_convertvector((f32x2{x, y}), h2); }
+
 // x less the low or the high half of h, in one instruction.
 __device__ __forceinline__ float less_low(float x, h2 h)
 {
@@ -136,23 +138,12 @@ struct DenseArgs {
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
-__device__ __forceinline__ float across_groups_max(float x)
-{
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
-}
-__device__ __forceinline__ float across_groups_sum(float x)
-{
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
-}
-
-// One row's 32 elements of a lane, scaled by a power of two that brings the row's largest into [2^13, 2^14), negated if
+// A lane's 8 NF elements of a row, which LANES lanes (64 / LANES apart) share, scaled by a power of two that brings the row's largest into [2^13, 2^14), negated if
 // asked and split into QP binary16 parts; returns the exponent that takes the scaling back.
-template <typename QT, int QP>
-__device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP][4])
+template <typename QT, int QP, int NF, int LANES>
+__device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP][NF])
 {
-    constexpr int NV = 32 * sizeof(QT) / 16;
+    constexpr int NV = 8 * NF * sizeof(QT) / 16;
     uint4 u[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) u[i] = reinterpret_cast<const uint4*>(q)[i];
@@ -172,13 +163,13 @@ __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP]
         for (int i = 0; i < NV; ++i)
             most = max(max(max(most, u[i].x & 0x7fffffffu), u[i].y & 0x7fffffffu), max(u[i].z & 0x7fffffffu, u[i].w & 0x7fffffffu));
     }
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16)));
-    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 32)));
+#pragma unroll
+    for (int off = 64 / LANES; off < 64; off <<= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), off)));
     // rows below 2^-113 are scaled as those at it; an infinity or a NaN makes the row's results NaN, however it is scaled
     const int ex = min(max(static_cast<int>(most >> 23) - 127, -113), 127);
     const float up = __uint_as_float(static_cast<uint32_t>(13 - ex + 127) << 23 | (negate ? 0x80000000u : 0u));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < NF; ++c) {
         h2 hi[4], lo[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -194,14 +185,42 @@ __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP]
             }
             x *= up;
             y *= up;
-            hi[j] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x, y));
+            hi[j] = to_half(x, y);
             lo[j] = hi[j];
-            if constexpr (QP == 2) lo[j] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(less_low(x, hi[j]), less_high(y, hi[j])));
+            if constexpr (QP == 2) lo[j] = to_half(less_low(x, hi[j]), less_high(y, hi[j]));
         }
         frag[0][c] = join(hi[0], hi[1], hi[2], hi[3]);
         if constexpr (QP == 2) frag[1][c] = join(lo[0], lo[1], lo[2], lo[3]);
     }
     return ex - 13;
+}
+
+constexpr int kWaves = kDenseWaves;
+static_assert(kWaves == kThreads / 64, "wavefronts of a workgroup");
+
+// Largest of 64 numbers that are not negative, by data-parallel-primitive moves.
+__device__ __forceinline__ int wave_max(int x)
+{
+#define SPOTLIGHT_DPP_MAX(ctrl, rows) x = max(x, __builtin_amdgcn_update_dpp(0, x, ctrl, rows, 0xf, true))
+    SPOTLIGHT_DPP_MAX(0x111, 0xf);   // row_shr:1
+    SPOTLIGHT_DPP_MAX(0x112, 0xf);   // row_shr:2
+    SPOTLIGHT_DPP_MAX(0x114, 0xf);   // row_shr:4
+    SPOTLIGHT_DPP_MAX(0x118, 0xf);   // row_shr:8
+    SPOTLIGHT_DPP_MAX(0x142, 0xa);   // lane 15 of rows 0 and 2 to rows 1 and 3
+    SPOTLIGHT_DPP_MAX(0x143, 0xc);   // lane 31 to rows 2 and 3
+#undef SPOTLIGHT_DPP_MAX
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
+__device__ __forceinline__ float across_groups_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float across_groups_sum(float x)
+{
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
 }
 
 // MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a split.
@@ -289,21 +308,24 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     const float* vs = a.v_scale + head * a.blocks;
     const uint32_t last_block = static_cast<uint32_t>(k0 + (n > 0 ? n - 1 : 0)) >> a.shift;   // tokens are below 2^31
 
-    // the largest scale of the run's values
-    float unit = 0.0f;
+    // the largest scale of the run's values, as bits; NaN is left out
+    int unit_bits = 0;
     if (n > 0)
-        for (uint32_t j = (static_cast<uint32_t>(k0) >> a.shift) + lane; j <= last_block; j += 64) unit = fmaxf(unit, vs[j]);
+        for (uint32_t j = (static_cast<uint32_t>(k0) >> a.shift) + lane; j <= last_block; j += 64) {
+            const int v = reinterpret_cast<const int*>(vs)[j];
+            unit_bits = max(unit_bits, v > kInf ? 0 : v);
+        }
     h8 qf[MT][QP][4];
     float factor[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int ex = load_row<QT, QP>(static_cast<const QT*>(a.q) + (head * a.rows + row[t]) * kHeadDim + g * 32, a.negate, qf[t]);
+        const int ex = load_row<QT, QP, 4, 4>(static_cast<const QT*>(a.q) + (head * a.rows + row[t]) * kHeadDim + g * 32, a.negate, qf[t]);
         factor[t] = ldexpf(a.scale2, ex);
     }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) unit = fmaxf(unit, __shfl_xor(unit, off));
-    if (!(unit > 0.0f)) unit = 1.0f;
-    const int unit_bits = __builtin_amdgcn_readfirstlane(__float_as_int(unit)) - ((127 + kVUp) << 23);
+    unit_bits = wave_max(unit_bits);
+    if (unit_bits == 0) unit_bits = 127 << 23;
+    const float to_value = ldexpf(__int_as_float(unit_bits), -kVUp);
+    unit_bits -= (127 + kVUp) << 23;
 
     f4 acc[MT][8];
     float base[MT], l[MT];                       // kPUp less the maximum (infinite: none yet), and the lane's sum of weights
@@ -406,8 +428,8 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             h2 h[4], r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                h[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(x[2 * e], x[2 * e + 1]));
-                r[e] = __builtin_bit_cast(h2, __builtin_amdgcn_cvt_pkrtz(less_low(x[2 * e], h[e]), less_high(x[2 * e + 1], h[e])));
+                h[e] = to_half(x[2 * e], x[2 * e + 1]);
+                r[e] = to_half(less_low(x[2 * e], h[e]), less_high(x[2 * e + 1], h[e]));
             }
             hi[t] = join(h[0], h[1], h[2], h[3]);
             lo[t] = join(r[0], r[1], r[2], r[3]);
@@ -458,7 +480,6 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     for (; s < steps; ++s) step(s, Flag<true>{});
 
     // the wavefronts' results, joined: lane (g, i) has columns 32g .. 32g+31 of row i
-    const float to_value = ldexpf(unit, -kVUp);
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const float sum = across_groups_sum(l[t]);

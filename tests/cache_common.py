@@ -112,7 +112,7 @@ def attention(q, k, v, seen, scale):
 
 def tolerance(mag, size, chain, q_parts=1, p_err=0.0):
     """How far a result may be off: every score by (128 + 8) roundings of its products' sum (and, where binary32 rows of q
-    are split in two binary16 parts, each cut to 11 bits, 2^-20 of them), which moves each weight by as much; the exponential by 2 units; p by
+    are split in two binary16 parts, each rounded to 11 bits, 2^-20 of them), which moves each weight by as much; the exponential by 2 units; p by
     p_err; sums by `chain` roundings.  Both the numerator and the denominator take the error."""
     u = 2.0 ** -24
     score = (136 * u + (2.0 ** -20 if q_parts == 2 else 0.0)) * size
@@ -120,7 +120,7 @@ def tolerance(mag, size, chain, q_parts=1, p_err=0.0):
 
 
 def split_floor(v):
-    """What the binary16 parts of the weights lose however small a weight is: a weight is scaled by 2^11, and of its second part
-    binary16 drops less than its smallest step, 2^-24.  So each key's weight (relative to the largest) is off by less than
-    2^-35, and a column's sum by at most 2^-35 sum |v|; the denominator is at least 1.  v: the head's values [n, d]."""
-    return 2.0 ** -35 * torch.nan_to_num(v).abs().sum(0)
+    """What the binary16 parts of the weights lose however small a weight is: a weight is scaled by 2^7, and of its second part
+    binary16 drops at most half its smallest step, 2^-25.  So each key's weight (relative to the largest) is off by at most
+    2^-32, and a column's sum by at most 2^-32 sum |v|; the denominator is at least 1.  v: the head's values [n, d]."""
+    return 2.0 ** -32 * torch.nan_to_num(v).abs().sum(0)

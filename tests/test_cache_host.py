@@ -169,6 +169,9 @@ int main()
                                 }
                                 ok = ok && (s.tiles == 1 ? runs * Hkv <= d.grid : (runs * Hkv + 7) / 8 * 8 * s.tiles <= d.grid);
                                 ok = ok && d.splits == (s.nsplit > 1) && (!d.splits || runs * Hkv * s.tiles * s.tile_rows <= p.dense_rows);
+                                const size_t from = p.off_dense_ml, to = p.off_dense_acc + p.dense_rows * 512;
+                                ok = ok && to <= p.total_bytes && p.off_dense_acc >= from + p.dense_rows * 8 && from % 256 == 0 && p.off_dense_acc % 256 == 0;
+                                ok = ok && ((from >= p.off_gcum && to <= p.off_wnorm) || from >= p.off_open_counts) && to <= std::max(p.off_runs, p.off_wnorm);
                                 ok = ok && (!d.joins || runs * Hkv * s.tiles <= kJoinGroups);
                                 for (const cache::FastDiv& f : {s.by_nsplit, s.by_heads, s.by_tiles8, s.by_most, s.by_spare})
                                     for (uint32_t x : {0u, 1u, f.d - 1, f.d, f.d + 1, 5 * f.d - 1, 5 * f.d, 99999u, (1u << 24) + 1, (1u << 31) - 1})
