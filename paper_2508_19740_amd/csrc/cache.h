@@ -10,6 +10,9 @@
 namespace spotlight {
 namespace cache {
 
+// The last-level cache.  Calls with as many bytes that nothing reads twice pass it by (non-temporal loads and stores).
+constexpr int64_t kCacheBytes = 256 << 20;
+
 // Division of numbers below 2^31 by one that the host knows.
 struct FastDiv {
     uint32_t d, mul, shift;

@@ -44,6 +44,23 @@ template <> struct Vec<float> {
 
 constexpr uint32_t kInfBits = 0x7f800000u;
 
+// Of kCacheBytes of rows and more, bfloat16, 32 heads of 131072 rows 558 -> 508 us, 16 of 65536 140 -> 125 us, binary32, 8 of 32768
+// 61 -> 54 us; of less, 8 of 32768 in bfloat16, 134 MB, 31.2 -> 32.3 us, and a smaller write that is read back at once
+// 21.2 -> 24.6 us.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const uint4* p)
+{
+    const u4 v = __builtin_nontemporal_load(reinterpret_cast<const u4*>(p));
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+__device__ __forceinline__ void store_once(uint32_t* p, uint32_t v) { __builtin_nontemporal_store(v, p); }
+__device__ __forceinline__ void store_once(uint2* p, uint2 v)
+{
+    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+    __builtin_nontemporal_store(u2{v.x, v.y}, reinterpret_cast<u2*>(p));
+}
+
 // kElems codes: one word or two
 template <int E> struct CodeWord;
 template <> struct CodeWord<4> { typedef uint32_t type; };
@@ -87,7 +104,7 @@ struct RowsArgs {
     int shift;                     // log2 of the tokens of a block
 };
 
-template <typename CT, typename XT, int TB>
+template <typename CT, typename XT, int TB, bool ONCE>
 __global__ __launch_bounds__(kThreads) void write_kernel(RowsArgs a)
 {
     constexpr int E = Vec<XT>::kElems;
@@ -118,7 +135,10 @@ __global__ __launch_bounds__(kThreads) void write_kernel(RowsArgs a)
             const int v = i * kThreads + tid;
             const int64_t row = r0 + v / VR;
             u[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (row >= lo && row < hi) u[i] = x[(row - start) * VR + v % VR];
+            if (row >= lo && row < hi) {
+                const uint4* from = x + (row - start) * VR + v % VR;
+                u[i] = ONCE ? load_once(from) : *from;
+            }
         }
 #pragma unroll
         for (int i = 0; i < IT; ++i) most = max(most, Vec<XT>::largest(u[i]));
@@ -173,7 +193,8 @@ __global__ __launch_bounds__(kThreads) void write_kernel(RowsArgs a)
                 uint32_t* w = reinterpret_cast<uint32_t*>(&c);
 #pragma unroll
                 for (int j = 0; j < E / 4; ++j) w[j] = encode4<CT>(f + 4 * j, inv, odd);
-                codes[r0 * VR + v] = c;
+                if constexpr (ONCE) store_once(codes + r0 * VR + v, c);
+                else codes[r0 * VR + v] = c;
             }
         }
         if (tid == 0) scale[blk] = poisoned ? __uint_as_float(0x7fc00000u) : power_of_two(ex);
@@ -186,11 +207,13 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi)
     return __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(lo), static_cast<__bf16>(hi)});
 }
 
-// Four vectors of 16 bytes a thread, loads first.
-template <typename CT, typename XT>
+// U vectors of 16 bytes a thread, loads first.  Beyond the last-level cache two measured best (32 heads of 131072 rows, bfloat16, with
+// 1 / 2 / 4 / 8: 525 / 540 / 560 / 564 us; 16 of 65536, binary32: 265 / 218 / 234 / 238 us), below it four (4 heads of 10007
+// rows just written, binary32, with 2 / 4: 12.5 / 10.3 us).
+template <typename CT, typename XT, int U>
 __global__ __launch_bounds__(kThreads) void read_kernel(RowsArgs a)
 {
-    constexpr int E = Vec<XT>::kElems, VR = kHeadDim / E, U = 4;
+    constexpr int E = Vec<XT>::kElems, VR = kHeadDim / E;
     typedef typename CodeWord<E>::type Codes;
     const int tid = threadIdx.x, z = blockIdx.z;
     if (!a.out[z]) return;
@@ -237,12 +260,39 @@ __global__ __launch_bounds__(kThreads) void read_kernel(RowsArgs a)
     }
 }
 
-template <typename CT, typename XT>
+template <typename CT, typename XT, bool ONCE>
 void launch_write_block(spotlight_ctx* ctx, const RowsArgs& a, int block, const dim3& grid)
 {
-    auto kern = block == 16 ? write_kernel<CT, XT, 16> : block == 32 ? write_kernel<CT, XT, 32>
-              : block == 64 ? write_kernel<CT, XT, 64> : write_kernel<CT, XT, 128>;
+    auto kern = block == 16 ? write_kernel<CT, XT, 16, ONCE> : block == 32 ? write_kernel<CT, XT, 32, ONCE>
+              : block == 64 ? write_kernel<CT, XT, 64, ONCE> : write_kernel<CT, XT, 128, ONCE>;
     hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, ctx->stream, a);
+}
+
+// Workgroups beyond this many take a second turn, so that a grid stays within the launch limits.
+constexpr int64_t kMaxGridX = 1 << 20;
+
+template <typename CT, typename XT>
+void launch_write(spotlight_ctx* ctx, const RowsArgs& a, int block, const dim3& grid)
+{
+    const int64_t bytes = 2 * a.n * ctx->plan.B * ctx->plan.Hkv * kHeadDim * static_cast<int64_t>(sizeof(XT));
+    if (bytes >= kCacheBytes) launch_write_block<CT, XT, true>(ctx, a, block, grid);
+    else launch_write_block<CT, XT, false>(ctx, a, block, grid);
+}
+
+template <typename CT, typename XT, int U>
+void launch_read_vectors(spotlight_ctx* ctx, const RowsArgs& a)
+{
+    const int64_t wgs = (a.n * (kHeadDim / Vec<XT>::kElems) + U * kThreads - 1) / (U * kThreads);
+    const dim3 grid(static_cast<unsigned>(wgs < kMaxGridX ? wgs : kMaxGridX), static_cast<unsigned>(ctx->plan.B * ctx->plan.Hkv), 2);
+    hipLaunchKernelGGL((read_kernel<CT, XT, U>), grid, dim3(kThreads), 0, ctx->stream, a);
+}
+
+template <typename CT, typename XT>
+void launch_read(spotlight_ctx* ctx, const RowsArgs& a)
+{
+    const int64_t bytes = 2 * a.n * ctx->plan.B * ctx->plan.Hkv * kHeadDim * static_cast<int64_t>(sizeof(XT));
+    if (bytes >= kCacheBytes) launch_read_vectors<CT, XT, 2>(ctx, a);
+    else launch_read_vectors<CT, XT, 4>(ctx, a);
 }
 
 RowsArgs rows_args(const spotlight_ctx* ctx, const spotlight_cache& c, int64_t t0, int64_t n, const int32_t* first, const int32_t* count)
@@ -265,9 +315,6 @@ RowsArgs rows_args(const spotlight_ctx* ctx, const spotlight_cache& c, int64_t t
     return a;
 }
 
-// Workgroups beyond this many take a second turn, so that a grid stays within the launch limits.
-constexpr int64_t kMaxGridX = 1 << 20;
-
 }  // namespace
 
 int launch_cache_write(spotlight_ctx* ctx, const spotlight_cache& c, const void* K, const void* V, int64_t t0, int64_t n,
@@ -282,11 +329,11 @@ int launch_cache_write(spotlight_ctx* ctx, const spotlight_cache& c, const void*
     const int64_t nblk = first ? (n + T - 2) / T + 1 : (t0 % T + n + T - 1) / T;
     const dim3 grid(static_cast<unsigned>(nblk < kMaxGridX ? nblk : kMaxGridX), static_cast<unsigned>(p.B * p.Hkv), 2);
     if (p.kv_dtype == SPOTLIGHT_BF16) {
-        if (c.code_type == SPOTLIGHT_E4M3) launch_write_block<E4M3, bf16_raw>(ctx, a, c.block_tokens, grid);
-        else launch_write_block<I8, bf16_raw>(ctx, a, c.block_tokens, grid);
+        if (c.code_type == SPOTLIGHT_E4M3) launch_write<E4M3, bf16_raw>(ctx, a, c.block_tokens, grid);
+        else launch_write<I8, bf16_raw>(ctx, a, c.block_tokens, grid);
     } else {
-        if (c.code_type == SPOTLIGHT_E4M3) launch_write_block<E4M3, float>(ctx, a, c.block_tokens, grid);
-        else launch_write_block<I8, float>(ctx, a, c.block_tokens, grid);
+        if (c.code_type == SPOTLIGHT_E4M3) launch_write<E4M3, float>(ctx, a, c.block_tokens, grid);
+        else launch_write<I8, float>(ctx, a, c.block_tokens, grid);
     }
     return hip_rc(hipGetLastError());
 }
@@ -297,12 +344,13 @@ int launch_cache_read(spotlight_ctx* ctx, const spotlight_cache& c, int64_t t0, 
     RowsArgs a = rows_args(ctx, c, t0, n, first, nullptr);
     a.out[0] = K;
     a.out[1] = V;
-    const int64_t vecs = n * (p.kv_dtype == SPOTLIGHT_BF16 ? kHeadDim / 8 : kHeadDim / 4);
-    const int64_t wgs = (vecs + 4 * kThreads - 1) / (4 * kThreads);
-    const dim3 grid(static_cast<unsigned>(wgs < kMaxGridX ? wgs : kMaxGridX), static_cast<unsigned>(p.B * p.Hkv), 2);
-    auto kern = p.kv_dtype == SPOTLIGHT_BF16 ? (c.code_type == SPOTLIGHT_E4M3 ? read_kernel<E4M3, bf16_raw> : read_kernel<I8, bf16_raw>)
-                                             : (c.code_type == SPOTLIGHT_E4M3 ? read_kernel<E4M3, float> : read_kernel<I8, float>);
-    hipLaunchKernelGGL(kern, grid, dim3(kThreads), 0, ctx->stream, a);
+    if (p.kv_dtype == SPOTLIGHT_BF16) {
+        if (c.code_type == SPOTLIGHT_E4M3) launch_read<E4M3, bf16_raw>(ctx, a);
+        else launch_read<I8, bf16_raw>(ctx, a);
+    } else {
+        if (c.code_type == SPOTLIGHT_E4M3) launch_read<E4M3, float>(ctx, a);
+        else launch_read<I8, float>(ctx, a);
+    }
     return hip_rc(hipGetLastError());
 }
 

@@ -225,3 +225,27 @@ def test_another_stream_and_a_graph():
     torch.cuda.synchronize()
     _same(host, cache)
     ctx.close()
+
+
+@pytest.mark.parametrize("code,kv,n", [("e4m3", "f32", 66001), ("i8", "bf16", 132003)])
+def test_more_than_the_last_level_cache(code, kv, n):
+    """Calls of over 256 MB of rows take other kernels: every code, scale and value.  (Whole blocks are new, so that the definition
+    needs no loop.)"""
+    b, hkv, block = 2, 2, 128
+    ctx = _ctx(b, hkv, n + 1 + block, kv)
+    cache = ctx.new_cache(cc.CODES[code], block)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rows = [(torch.randn(b, hkv, n, cc.D, generator=g, device=DEV) * torch.exp(torch.randn(b, hkv, n, 1, generator=g, device=DEV))).to(cc.KV[kv]) for _ in "kv"]
+    ctx.cache_write(cache, *rows, block)
+    got = ctx.cache_read(cache, n, block)
+    for x, y, back in zip("kv", rows, got):
+        y = torch.cat([y.double(), torch.zeros(b, hkv, -n % block, cc.D, dtype=torch.float64, device=DEV)], 2).view(b, hkv, -1, block, cc.D)
+        a = y.abs().amax((3, 4))
+        s = torch.tensor([cc.least_scale(v, code) for v in a.flatten().tolist()], dtype=torch.float64, device=DEV).view(a.shape)
+        assert torch.equal(getattr(cache, x + "_scale")[:, :, 1:].double(), s)
+        want = cc.nearest((y / s[..., None, None]).cpu(), code).to(DEV)      # (torch.ldexp is exact on the host)
+        assert torch.equal(getattr(cache, x).view(torch.uint8)[:, :, block:block + n].view(cc.CODES[code]).double(), want.view(b, hkv, -1, cc.D)[:, :, :n])
+        assert torch.equal(back.double(), (want * s[..., None, None]).view(b, hkv, -1, cc.D)[:, :, :n])
+        assert int(getattr(cache, x).view(torch.uint8)[:, :, :block].max()) == 0 and int(getattr(cache, x).view(torch.uint8)[:, :, block + n:].max()) == 0
+        del y, want
+    ctx.close()
