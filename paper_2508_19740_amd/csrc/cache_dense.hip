@@ -223,11 +223,12 @@ __device__ __forceinline__ float across_groups_sum(float x)
     return x + __shfl_xor(x, 32);
 }
 
-// MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a split.
-template <typename CT, typename QT, int MT>
+// MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a run.  ONCE: no other workgroup reads them.
+template <typename CT, typename QT, int MT, bool ONCE>
 __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(DenseArgs a)
 {
     constexpr int QP = sizeof(QT) == 2 ? 1 : 2;
+    constexpr int kAux = ONCE ? 2 : 0;           // non-temporal
     typedef Operand<CT> Op;
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     __shared__ float s_acc[kWaves][16][kHeadDim + 4];
@@ -289,7 +290,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + (t * (16 * kHeadDim) + j * 16), 0, 0);
+                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + (t * (16 * kHeadDim) + j * 16), 0, kAux);
         koff += kStep * kHeadDim;
     };
     auto load_v = [&]() {
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                vreg[t][r] = __builtin_amdgcn_raw_buffer_load_b64(vr, voff + (t * (16 * kHeadDim) + r * kHeadDim), 0, 0);
+                vreg[t][r] = __builtin_amdgcn_raw_buffer_load_b64(vr, voff + (t * (16 * kHeadDim) + r * kHeadDim), 0, kAux);
         voff += kStep * kHeadDim;
     };
     // on their way while the queries and scales are read
@@ -513,10 +514,15 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
                                 a.out + (head * a.rows + r0) * kHeadDim, reinterpret_cast<f32x2*>(&s_acc[0][0][0]));
 }
 
+// Codes that no other workgroup reads and no cache would hold until the next call: 268 MB, 32 / 8 heads 50.4 -> 45.3 us, with
+// lengths of their own, 28 / 4 heads 57.2 -> 52.3 us, 1074 MB 189 -> 162 us; but 134 MB, called again, 27.3 -> 29.4 us.
 template <typename CT, typename QT>
 void launch_mt(StageTimer& timer, const DenseArgs& a, const DensePlan& d)
 {
-    auto kern = d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1> : cache_dense_kernel<CT, QT, 2>;
+    const int64_t bytes = 2 * a.n_tokens * kHeadDim * a.shares.batch * a.shares.by_heads.d;
+    const bool once = a.shares.tiles == 1 && bytes >= kCacheBytes;
+    auto kern = once ? (d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1, true> : cache_dense_kernel<CT, QT, 2, true>)
+                     : (d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1, false> : cache_dense_kernel<CT, QT, 2, false>);
     timer.launch(kern, dim3(d.grid), dim3(kThreads), 0, a);
 }
 

@@ -311,3 +311,32 @@ def test_small_calls_one_after_the_other(hq, hkv, n, nq):
     want, mag, size = _dense(host, qs[1].cpu(), n, None, 0, 0, hq // hkv, nq)
     _check(first[4][0, 0], want, cc.tolerance(mag, size, 32 + n // 8, 1, 2.0 ** -20) + cc.split_floor(host.values("v")[0, 0]), "first")
     ctx.close()
+
+
+@pytest.mark.parametrize("nq,code,kv", [(1, "e4m3", "bf16"), (2, "i8", "f32"), (9, "i8", "bf16")])
+def test_more_than_the_last_level_cache(nq, code, kv):
+    """Over 256 MB of codes take other kernels."""
+    b, hkv, n, block, group = 2, 2, 262181, 64, 2
+    g = torch.Generator(device=DEV).manual_seed(31)
+    ctx = _ctx(b, group * hkv, hkv, n, 1, kv)
+    cache = ctx.new_cache(cc.CODES[code], block)
+    vals = {}
+    for x in "kv":
+        codes, scale = getattr(cache, x), getattr(cache, x + "_scale")
+        codes.copy_((torch.randn(codes.shape, generator=g, device=DEV) * 30).clamp(-120, 120).to(codes.dtype))
+        scale.copy_(torch.randint(-6, -3, scale.shape, generator=g, device=DEV).float().exp2())
+        vals[x] = codes, scale.cpu().double()
+        assert torch.equal(torch.frexp(vals[x][1])[0], torch.full_like(vals[x][1], 0.5))
+    q = _q(5, kv, b, group * hkv, nq)
+    lens = torch.tensor([n, n - 100003], dtype=torch.int32)
+    for ld in (None, lens):
+        out = ctx.dense_decode_cache(q.to(DEV), cache, n, None if ld is None else ld.to(DEV), SCALE)
+        for i in range(b):
+            ln = n if ld is None else int(ld[i])
+            seen = (torch.arange(ln)[None] <= (ln - nq + torch.arange(nq))[:, None]).repeat(group, 1)
+            for h in range(hkv):
+                k, v = (vals[x][0][i, h, :ln].cpu().double() * vals[x][1][i, h].repeat_interleave(block)[:ln, None] for x in "kv")
+                want, mag, size = cc.attention(q[i, group * h:group * (h + 1)].reshape(-1, cc.D), k, v, seen, SCALE)
+                _check(out[i, group * h:group * (h + 1)].reshape(-1, cc.D), want,
+                       cc.tolerance(mag, size, 32 + n // 8, 2 if kv == "f32" else 1, 2.0 ** -20) + cc.split_floor(v), f"batch {i} head {h}")
+    ctx.close()
