@@ -310,7 +310,8 @@ typedef struct {
  *   K, V   [B, Hkv, n_new, d]   kv_dtype
  *   first  [B]                  int32, device, or NULL
  *   count  [B]                  int32, device, or NULL
- * Errors: INVALID_ARG for a bad cache, t0 or n_new outside 0 .. Nmax, or (first NULL) t0 + n_new > Nmax.
+ * No rows (n_new 0) is no work; K and V may be NULL then.
+ * Errors: INVALID_ARG for a bad cache, K or V misaligned (16 bytes), t0 or n_new outside 0 .. Nmax, or (first NULL) t0 + n_new > Nmax.
  */
 int spotlight_cache_write(spotlight_ctx *ctx, const spotlight_cache *cache, const void *K, const void *V, int64_t t0,
                           int64_t n_new, const int32_t *first, const int32_t *count);
@@ -320,7 +321,7 @@ int spotlight_cache_write(spotlight_ctx *ctx, const spotlight_cache *cache, cons
  * above the type's largest becomes infinite).  Rows outside 0 .. Nmax-1 become zeros.
  *   K, V   [B, Hkv, n, d]   kv_dtype, written; either may be NULL
  *   first  [B]              int32, device, or NULL (0)
- * Errors: INVALID_ARG for a bad cache, both outputs NULL, t0 or n outside 0 .. Nmax, or (first NULL) t0 + n > Nmax.
+ * Errors: INVALID_ARG for a bad cache, both outputs NULL (n not 0) or one misaligned, t0 or n outside 0 .. Nmax, or (first NULL) t0 + n > Nmax.
  */
 int spotlight_cache_read(spotlight_ctx *ctx, const spotlight_cache *cache, int64_t t0, int64_t n, const int32_t *first,
                          void *K, void *V);

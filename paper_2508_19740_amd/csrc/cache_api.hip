@@ -48,7 +48,7 @@ extern "C" {
 int spotlight_cache_write(spotlight_ctx* ctx, const spotlight_cache* cache, const void* K, const void* V, int64_t t0,
                           int64_t n_new, const int32_t* first, const int32_t* count)
 {
-    if (!ctx || !K || !V) return SPOTLIGHT_ERR_INVALID_ARG;
+    if (!ctx || (n_new != 0 && (!K || !V))) return SPOTLIGHT_ERR_INVALID_ARG;
     int rc = check_cache(cache);
     if (rc != SPOTLIGHT_OK) return rc;
     rc = check_rows(ctx->plan, t0, n_new, first);
@@ -63,7 +63,7 @@ int spotlight_cache_write(spotlight_ctx* ctx, const spotlight_cache* cache, cons
 int spotlight_cache_read(spotlight_ctx* ctx, const spotlight_cache* cache, int64_t t0, int64_t n, const int32_t* first,
                          void* K, void* V)
 {
-    if (!ctx || (!K && !V)) return SPOTLIGHT_ERR_INVALID_ARG;
+    if (!ctx || (n != 0 && !K && !V)) return SPOTLIGHT_ERR_INVALID_ARG;
     int rc = check_cache(cache);
     if (rc != SPOTLIGHT_OK) return rc;
     rc = check_rows(ctx->plan, t0, n, first);
@@ -104,7 +104,7 @@ int spotlight_dense_decode_cache(spotlight_ctx* ctx, const void* q, const spotli
 int spotlight_hash_rows(spotlight_ctx* ctx, const void* K, const spotlight_hash_weights* w, int64_t t0, int64_t n_new,
                         uint32_t* codes)
 {
-    if (!ctx || !K || !codes) return SPOTLIGHT_ERR_INVALID_ARG;
+    if (!ctx || (n_new != 0 && !K) || !codes) return SPOTLIGHT_ERR_INVALID_ARG;
     const Plan& p = ctx->plan;
     int rc = check_weights(ctx, w);
     if (rc != SPOTLIGHT_OK) return rc;

@@ -76,6 +76,11 @@ int main()
         WANT(SPOTLIGHT_OK, spotlight_cache_write(&ctx, &good, mem, mem, 1000, 0, first, nullptr));
         WANT(SPOTLIGHT_OK, spotlight_cache_read(&ctx, &good, 1000, 0, first, mem, mem));
     }
+    // an empty tensor has no address
+    WANT(SPOTLIGHT_OK, spotlight_cache_write(&ctx, &good, nullptr, nullptr, 5, 0, nullptr, nullptr));
+    WANT(SPOTLIGHT_OK, spotlight_cache_read(&ctx, &good, 5, 0, nullptr, nullptr, nullptr));
+    WANT(SPOTLIGHT_OK, spotlight_hash_rows(&ctx, nullptr, &w, 5, 0, u));
+    WANT(bad, spotlight_cache_write(&ctx, &good, nullptr, nullptr, 1001, 0, nullptr, nullptr));
     WANT(bad, spotlight_cache_write(&ctx, &good, mem, mem, 999, 2, nullptr, nullptr));
     WANT(bad, spotlight_cache_read(&ctx, &good, 999, 2, nullptr, mem, mem));
     WANT(bad, spotlight_cache_read(&ctx, &good, 0, 1, nullptr, nullptr, nullptr));

@@ -249,3 +249,17 @@ def test_more_than_the_last_level_cache(code, kv, n):
         assert int(getattr(cache, x).view(torch.uint8)[:, :, :block].max()) == 0 and int(getattr(cache, x).view(torch.uint8)[:, :, block + n:].max()) == 0
         del y, want
     ctx.close()
+
+
+def test_no_rows():
+    """Writing and reading nothing is no work, and no error."""
+    ctx = _ctx(2, 2, 100)
+    cache = ctx.new_cache(torch.int8, 32)
+    K = torch.ones(2, 2, 40, 128, dtype=torch.bfloat16, device=DEV)
+    ctx.cache_write(cache, K, K)
+    before = cache.k.clone(), cache.k_scale.clone()
+    ctx.cache_write(cache, K[:, :, :0], K[:, :, :0], 40)
+    assert torch.equal(cache.k, before[0]) and torch.equal(cache.k_scale, before[1])
+    k, v = ctx.cache_read(cache, 0, 40)
+    assert k.shape == v.shape == (2, 2, 0, 128)
+    ctx.close()
