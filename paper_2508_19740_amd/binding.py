@@ -113,7 +113,8 @@ _CODE_TYPES = {torch.float8_e4m3fn: E4M3, torch.int8: I8}
 class Cache:
     """A key-value cache held in 8 bits: codes k, v [B, Hkv, Nmax, d] (torch.float8_e4m3fn or torch.int8)
     and k_scale, v_scale [B, Hkv, ceil(Nmax / block_tokens)] (float32 powers of two); a value is
-    code * scale.  Spotlight.new_cache makes an empty one."""
+    code * scale.  Spotlight.new_cache makes an empty one.  It holds these tensors for good: their
+    contents may change, their storage may not."""
 
     def __init__(self, k, v, k_scale, v_scale, block_tokens: int):
         if block_tokens not in (16, 32, 64, 128):
@@ -129,7 +130,13 @@ class Cache:
                 raise ValueError(f"{name}: want contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
         self._args = CacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _CODE_TYPES[k.dtype], block_tokens)
+        self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
         self._ref = C.byref(self._args)
+
+    def __setattr__(self, name, value):
+        if "_ref" in self.__dict__:
+            raise AttributeError(f"{name}: a Cache keeps its tensors; make another one")
+        object.__setattr__(self, name, value)
 
 
 def _dtype_code(t: torch.dtype) -> int:
@@ -342,6 +349,8 @@ class Spotlight:
             raise TypeError("cache: want a Cache")
         if cache.k.shape != self._kv_shape or cache.k.device != self.device:
             raise ValueError(f"cache: want {self._kv_shape} on {self.device}, got {tuple(cache.k.shape)} on {cache.k.device}")
+        if (cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(), cache.v_scale.data_ptr()) != cache._ptrs:
+            raise ValueError("cache: its tensors have other storage now; make another Cache")
         return cache._ref
 
     def _per_entry(self, t, name):

@@ -2,6 +2,7 @@
 on a context made on the host, the rule that splits keys over workgroups, the binding's checks."""
 import os
 import subprocess
+import types
 
 import pytest
 import torch
@@ -225,6 +226,24 @@ def test_cache_takes_matching_tensors():
 def test_cache_refuses_other_tensors(change):
     with pytest.raises(ValueError):
         sp.Cache(*change(_tensors()))
+
+
+def test_a_cache_keeps_its_tensors():
+    """The calls take the addresses that a Cache was made with: other tensors, or other storage, are refused."""
+    cache = sp.Cache(*_tensors(), 32)
+    for name in ("k", "v", "k_scale", "v_scale", "block_tokens"):
+        with pytest.raises(AttributeError):
+            setattr(cache, name, getattr(cache, name))
+    ctx = types.SimpleNamespace(_kv_shape=tuple(cache.k.shape), device=cache.k.device)
+    assert sp.Spotlight._cache(ctx, cache) is not None
+    cache.v_scale.fill_(2.0)
+    assert sp.Spotlight._cache(ctx, cache) is not None
+    for name in ("k", "v", "k_scale", "v_scale"):
+        other = sp.Cache(*_tensors(), 32)
+        t = getattr(other, name)
+        t.data = t.data.clone()
+        with pytest.raises(ValueError):
+            sp.Spotlight._cache(ctx, other)
 
 
 def test_the_reference_quantises_to_the_nearest_code():
