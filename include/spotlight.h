@@ -119,7 +119,8 @@ size_t spotlight_workspace_bytes(const spotlight_config *cfg);
  * lists (about one byte per (query head, token)), the partial attention results, a bit per key and
  * norms of the hash weights for bulk hashing (a second copy of bfloat16 weights that do not fit into
  * LDS), room for one copy of the hash weights (spotlight_prepack_weights), and for the partial results of
- * attention over the whole of an 8-bit cache (8.1 MiB, less for short caches). */
+ * attention over the whole of an 8-bit cache (8.1 MiB, less for short caches, more from 8193 query heads on; they lie
+ * over retrieval's scratch memory where that is large enough). */
 int spotlight_create(spotlight_ctx **out, const spotlight_config *cfg);
 
 /* Waits for the stream, frees the workspace and the context.  NULL is accepted. */
@@ -343,10 +344,11 @@ int spotlight_sparse_decode_cache(spotlight_ctx *ctx, const void *q, const spotl
  *   q     [B, Hq, n_q, d]  kv_dtype
  *   lens  [B]              int32, device, or NULL
  *   out   [B, Hq, n_q, d]  float32
- * The call enqueues two kernels, or one where the keys need no splitting, and nothing else.
- * Errors: INVALID_ARG for a bad cache or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax; UNSUPPORTED for more than
- * 2^24 / (Hq / Hkv) queries, or if more than 2^25 tokens would have to be split further than the workspace allows for
- * (over 16384 / ceil(n_tokens / 2^25) rows of q).
+ * The call enqueues two kernels, or one where the keys need no splitting and in small calls, and nothing else.
+ * Errors: INVALID_ARG for a bad cache, a misaligned q (16 bytes) or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax;
+ * UNSUPPORTED for more than 2^24 / (Hq / Hkv) queries, for 2^24 or more tiles of 32 rows (of B x Hkv x (Hq / Hkv) n_q), or if
+ * more than 2^25 tokens would have to be split further than the workspace allows for (over 16384 / ceil(n_tokens / 2^25) rows of q;
+ * with lens, also where a share of all sequences' tokens would be as long).
  */
 int spotlight_dense_decode_cache(spotlight_ctx *ctx, const void *q, const spotlight_cache *cache, int64_t n_tokens,
                                  int32_t n_q, const int32_t *lens, float scale, float *out);

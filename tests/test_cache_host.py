@@ -115,6 +115,11 @@ int main()
     WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::plan_dense(ctx.plan, 256, 100, (1 << 24) + 1, nullptr, &d));
     WANT(SPOTLIGHT_OK, cache::plan_dense(ctx.plan, 256, 1L << 27, 1, nullptr, &d));
     WANT(SPOTLIGHT_OK, cache::plan_dense(ctx.plan, 256, 1L << 27, 1, i, &d));
+    // a launch's threads are counted in 32 bits
+    const spotlight_config wide = config(8, 64, 64, 1L << 20, 50);
+    if (make_plan(&wide, &ctx.plan) != SPOTLIGHT_OK) return 2;
+    WANT(SPOTLIGHT_ERR_UNSUPPORTED, cache::plan_dense(ctx.plan, 256, 100, 1 << 20, nullptr, &d));
+    WANT(SPOTLIGHT_OK, cache::plan_dense(ctx.plan, 256, 100, (1 << 20) - 32, nullptr, &d));
     return failed;
 }
 """

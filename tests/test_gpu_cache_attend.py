@@ -340,3 +340,25 @@ def test_more_than_the_last_level_cache(nq, code, kv):
                 _check(out[i, group * h:group * (h + 1)].reshape(-1, cc.D), want,
                        cc.tolerance(mag, size, 32 + n // 8, 2 if kv == "f32" else 1, 2.0 ** -20) + cc.split_floor(v), f"batch {i} head {h}")
     ctx.close()
+
+
+@pytest.mark.parametrize("hq,hkv,n,nq", [(1, 1, 300, 1), (2, 2, 4000, 1), (8, 2, 4000, 1), (8, 2, 4000, 9), (1, 1, 60, 2)])
+def test_results_at_any_element(hq, hkv, n, nq):
+    """`out` is float32 at any address; what lies around it stays."""
+    host = cc.random_cache(1, hkv, n, 64, "i8", 2)
+    ctx, cache = _ctx(1, hq, hkv, n, min(n, 600)), host.device()
+    q = _q(9, "bf16", 1, hq, nq).to(DEV)
+    idx = torch.randint(0, n, (1, hq, min(n, 600)), dtype=torch.int32, device=DEV)
+    size = hq * nq * cc.D
+    for at in (1, 2, 3, 5):
+        buf = torch.full((size + 8,), 7.0, device=DEV)
+        out = buf[at:at + size].view(1, hq, nq, cc.D)
+        ctx.dense_decode_cache(q, cache, n, out=out)
+        assert torch.equal(out, ctx.dense_decode_cache(q, cache, n))
+        assert bool((buf[:at] == 7).all()) and bool((buf[at + size:] == 7).all())
+        if nq == 1:
+            out.fill_(7.0)
+            ctx.sparse_decode_cache(q[:, :, 0], cache, idx, out=out[:, :, 0])
+            assert torch.equal(out[:, :, 0], ctx.sparse_decode_cache(q[:, :, 0], cache, idx))
+            assert bool((buf[:at] == 7).all()) and bool((buf[at + size:] == 7).all())
+    ctx.close()
