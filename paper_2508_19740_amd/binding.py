@@ -130,7 +130,10 @@ class Cache:
                 raise ValueError(f"{name}: want contiguous {dtype} {tuple(shape)} on {k.device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
         self.k, self.v, self.k_scale, self.v_scale, self.block_tokens = k, v, k_scale, v_scale, block_tokens
         self._args = CacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _CODE_TYPES[k.dtype], block_tokens)
-        self._ptrs = (k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr())
+        # what every call compares: the shape as it was, and where the tensors lie now
+        self._shape, self._device = tuple(k.shape), k.device
+        self._at = (k.data_ptr, v.data_ptr, k_scale.data_ptr, v_scale.data_ptr)
+        self._ptrs = tuple(at() for at in self._at)
         self._ref = C.byref(self._args)
 
     def __setattr__(self, name, value):
@@ -347,9 +350,10 @@ class Spotlight:
     def _cache(self, cache: Cache):
         if not isinstance(cache, Cache):
             raise TypeError("cache: want a Cache")
-        if cache.k.shape != self._kv_shape or cache.k.device != self.device:
-            raise ValueError(f"cache: want {self._kv_shape} on {self.device}, got {tuple(cache.k.shape)} on {cache.k.device}")
-        if (cache.k.data_ptr(), cache.v.data_ptr(), cache.k_scale.data_ptr(), cache.v_scale.data_ptr()) != cache._ptrs:
+        if cache._shape != self._kv_shape or cache._device != self.device:
+            raise ValueError(f"cache: want {self._kv_shape} on {self.device}, got {cache._shape} on {cache._device}")
+        k, v, ks, vs = cache._at
+        if (k(), v(), ks(), vs()) != cache._ptrs:
             raise ValueError("cache: its tensors have other storage now; make another Cache")
         return cache._ref
 
