@@ -66,13 +66,11 @@ template <> struct Operand<E4M3> {
     static __device__ __forceinline__ Ratio ratio(float r) { return r; }
     static __device__ __forceinline__ void columns(uint32_t a, uint32_t b, Ratio r, h2 (&o)[4])
     {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const h2 x = j ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, r, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, r, false);
-            const h2 y = j ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, r, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, r, false);
-            o[2 * j] = h2{x.x, y.x};
-            o[2 * j + 1] = h2{x.y, y.y};
-        }
+        const uint32_t lo = __builtin_amdgcn_perm(b, a, 0x05010400u), hi = __builtin_amdgcn_perm(b, a, 0x07030602u);
+        o[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, r, false);
+        o[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, r, true);
+        o[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, r, false);
+        o[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, r, true);
     }
 };
 template <> struct Operand<I8> {
