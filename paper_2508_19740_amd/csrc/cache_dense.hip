@@ -1,8 +1,7 @@
 // Attention of the last n_q tokens of each sequence over the whole 8-bit cache.
 //
 // The rows of a key-value head are its G query heads times n_q queries, contiguous in q.  A wavefront
-// takes tiles of 16 rows and a run of keys, 32 keys a step, and needs neither LDS nor a barrier until its
-// keys are done:
+// takes tiles of 16 rows and a run of keys, 32 keys a step, and needs no barrier until its keys are done:
 //
 //   S^T = K Q^T     v_mfma_f32_16x16x32_f16.  Lane (g, i) = (lane / 16, lane % 16) loads 32 adjacent
 //                   bytes of key i; four products take 8 of them each, and q lies in registers in the
@@ -227,9 +226,10 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
 {
     constexpr int QP = sizeof(QT) == 2 ? 1 : 2;
     constexpr int kAux = ONCE ? 2 : 0;           // non-temporal
+    constexpr bool TURN = MT == 1 && QP == 1;    // keys pass through LDS (below)
     typedef Operand<CT> Op;
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-    __shared__ float s_acc[kWaves][16][kHeadDim + 4];
+    __shared__ alignas(16) float s_acc[kWaves][16][kHeadDim + 4];
     __shared__ uint32_t s_before;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -280,16 +280,46 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     const int64_t start = (head * a.Nmax + k0) * kHeadDim;
     const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.k + start), 0, n * kHeadDim, 0x00020000);
     const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.v + start), 0, n * kHeadDim, 0x00020000);
-    u4 kreg[2][2];
+    u4 kreg[2][2];                               // lane (g, i): 32 bytes of the keys i and 16 + i
     u2 vreg[2][4];
-    int koff = i * kHeadDim + g * 32, voff = g * (4 * kHeadDim) + i * 8;      // of the next step
+    int koff = TURN ? lane * 16 : i * kHeadDim + g * 32, voff = g * (4 * kHeadDim) + i * 8;      // of the next step
+    // Loaded like that, neighbouring lanes read different rows: 64 accesses of the vector cache an instruction.  With TURN an
+    // instruction reads eight whole rows, a step further ahead, and the lanes exchange them through 4 KB of LDS that the
+    // wavefront has to itself (its place for results): 16 bytes of row r at place (chunk ^ r % 8), without bank conflicts either
+    // way.  Half as many cache accesses: 268 MB, 32 / 8 heads 50.6 -> 49.4 us, lengths of their own, 28 / 4 heads 57.6 -> 56.2 us.
+    // With 32 rows vector and matrix instructions are the bound (112.4 -> 111.8 us), and binary32 queries leave too few registers.
+    u4 kraw[TURN ? 4 : 1];
+    uint8_t* const stage = reinterpret_cast<uint8_t*>(&s_acc[wave][0][0]);
+    uint8_t* const put = stage + (lane >> 3) * kHeadDim + ((lane ^ lane >> 3) & 7) * 16;
+    const int get = i * kHeadDim + ((2 * g ^ i) & 7) * 16;
     auto load_k = [&]() {
+        if constexpr (TURN) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 4; ++t) kraw[t] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + t * (8 * kHeadDim), 0, kAux);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-                kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + (t * (16 * kHeadDim) + j * 16), 0, kAux);
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    kreg[t][j] = __builtin_amdgcn_raw_buffer_load_b128(kr, koff + (t * (16 * kHeadDim) + j * 16), 0, kAux);
+        }
         koff += kStep * kHeadDim;
+    };
+    // The keys of the next step, and loads of those behind them.  (LDS serves a wavefront in order: it needs no wait.)
+    auto next_k = [&]() {
+        if constexpr (TURN) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) *reinterpret_cast<u4*>(put + t * (8 * kHeadDim)) = kraw[t];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) kreg[t][j] = *reinterpret_cast<const u4*>(stage + (get ^ 16 * j) + t * (16 * kHeadDim));
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+        load_k();
     };
     auto load_v = [&]() {
 #pragma unroll
@@ -347,6 +377,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
         }
     };
     if (steps > 0) load_scales(0);
+    if constexpr (TURN) next_k();
 
     auto step = [&](int s, auto masked) {
         // the scales of this step; the next one's are on their way from here on
@@ -384,7 +415,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
 #pragma unroll
                     for (int p = 0; p < QP; ++p) sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][kt], 0, 0, 0);
             }
-        load_k();
+        next_k();
         // softmax
         h8 hi[MT], lo[MT];
 #pragma unroll
