@@ -362,3 +362,45 @@ def test_results_at_any_element(hq, hkv, n, nq):
             assert torch.equal(out[:, :, 0], ctx.sparse_decode_cache(q[:, :, 0], cache, idx))
             assert bool((buf[:at] == 7).all()) and bool((buf[at + size:] == 7).all())
     ctx.close()
+
+
+@pytest.mark.parametrize("nq", [1, 9])
+def test_offsets_beyond_32_bits(nq):
+    """4 GiB of codes a head: keys of zeros (weight 1 each) and a few, spread over the cache, that take most of the weight."""
+    n, block, hq = (1 << 25) + 77, 128, 2
+    ctx = _ctx(1, hq, 1, n, 300)
+    cache = ctx.new_cache(torch.float8_e4m3fn, block)
+    cache.v.view(torch.uint8).random_(0, 120, generator=torch.Generator(device=DEV).manual_seed(1))
+    cache.k_scale.fill_(2.0 ** -6)
+    cache.v_scale.fill_(2.0 ** -6)
+    q = _q(8, "bf16", 1, 1, 1)
+    q = torch.cat([(q * (1.0 + 0.01 * (h + i))).to(q.dtype) for h in range(hq) for i in range(nq)], 2).view(1, hq, nq, cc.D)
+    at = torch.tensor([0, 1, 127, 128, 5000, (1 << 24) - 1, 1 << 24, (1 << 24) + 1, 3 << 23, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, n - 20, n - 12])
+    rows = torch.sign(q[0, 0, 0].float())[None] * torch.linspace(176, 208, len(at))[:, None]
+    cache.k[0, 0, at.to(DEV)] = rows.to(DEV).to(torch.float8_e4m3fn)
+    k = cache.k[0, 0, at.to(DEV)].cpu().double() * 2.0 ** -6
+    v = cache.v[0, 0, at.to(DEV)].cpu().double() * 2.0 ** -6
+    total = torch.zeros(cc.D, dtype=torch.float64)                              # of all values (codes 0 .. 119 are positive)
+    for a in range(0, n - nq + 1, 1 << 20):
+        total += cache.v[0, 0, a:min(a + (1 << 20), n - nq + 1)].double().sum(0).cpu() * 2.0 ** -6
+    tail = cache.v[0, 0, n - nq + 1:].cpu().double() * 2.0 ** -6
+    out = ctx.dense_decode_cache(q.to(DEV), cache, n)
+    for h in range(hq):
+        for i in range(nq):
+            s = (q[0, h, i].double() @ k.T) * SCALE
+            w, sees = torch.exp(s), n - nq + 1 + i
+            want = (total + tail[:i].sum(0) + (w - 1) @ v) / (sees + (w - 1).sum())
+            size = (SCALE * (q[0, h, i].double().abs() @ k.abs().T)).max()
+            # a wavefront sums at most n / 2048 keys and 32 more (four of them in each of 512 runs), and then come the runs
+            tol = cc.tolerance(want, size, n // 2048 + 32 + 512, 1, 2.0 ** -20) + 2.0 ** -32 * total
+            _check(out[0, h, i], want, tol, f"head {h} query {i}")
+    if nq == 1:
+        idx = torch.cat([at, torch.randint(0, n, (300 - len(at),), generator=torch.Generator().manual_seed(2))])
+        idx = idx[torch.randperm(300, generator=torch.Generator().manual_seed(3))].int().repeat(1, hq, 1)
+        got = ctx.sparse_decode_cache(q[:, :, 0].contiguous().to(DEV), cache, idx.to(DEV))
+        where = idx[0, 0].long().to(DEV)
+        kk, vv = (getattr(cache, x)[0, 0, where].cpu().double() * 2.0 ** -6 for x in "kv")
+        for h in range(hq):
+            want, mag, size = cc.attention(q[0, h], kk, vv, torch.ones(1, 300, dtype=torch.bool), SCALE)
+            _check(got[0, h][None], want, cc.tolerance(mag, size, 64), f"gathered, head {h}")
+    ctx.close()
