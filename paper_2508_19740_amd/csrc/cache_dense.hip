@@ -17,7 +17,8 @@
 //
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
-//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).
+//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).  Their sums are
+//       kept apart and meet in the score less the maximum: in one sum every step would round off (5e-7 of the result, 3.3e-7 now).
 //   p   is in [0, 2^8] (below), scaled by 2^7 and split in two parts: 22 bits, or 2^-32 of the largest weight
 //       where that is more.  Both are rounded to nearest: what many small weights lose must not add up.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
@@ -402,9 +403,11 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             nan_values = __any(found != 0);
         }
         // scores
-        f4 sc[MT][2];
+        f4 sc[MT][QP][2];                                       // of each part of q: sums of the large one are nearly exact
 #pragma unroll
-        for (int t = 0; t < MT; ++t) sc[t][0] = sc[t][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int p = 0; p < QP; ++p) sc[t][p][0] = sc[t][p][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -413,7 +416,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int p = 0; p < QP; ++p) sc[t][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][kt], 0, 0, 0);
+                    for (int p = 0; p < QP; ++p) sc[t][p][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][p][kt], 0, 0, 0);
             }
         next_k();
         // softmax
@@ -423,10 +426,15 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             float f[2], x[8];
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt) f[kt] = factor[t] * kscale[kt];
+            // the large part and the number first: where the weight is large they nearly cancel, and little is rounded off
+            auto score = [&](int e, float add) {
+                const float y = __builtin_fmaf(sc[t][0][e / 4][e % 4], f[e / 4], add);
+                return QP == 2 ? __builtin_fmaf(sc[t][QP - 1][e / 4][e % 4], f[e / 4], y) : y;
+            };
             float top = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                x[e] = __builtin_fmaf(sc[t][e / 4][e % 4], f[e / 4], base[t]);
+                x[e] = score(e, base[t]);
                 if constexpr (decltype(masked)::value)
                     if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
                 top = fmaxf(top, x[e]);
@@ -435,7 +443,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
                 float high = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    x[e] = sc[t][e / 4][e % 4] * f[e / 4];
+                    x[e] = score(e, -0.0f);
                     if constexpr (decltype(masked)::value)
                         if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
                     high = fmaxf(high, x[e]);
