@@ -346,7 +346,7 @@ int spotlight_sparse_decode_cache(spotlight_ctx *ctx, const void *q, const spotl
  *   out   [B, Hq, n_q, d]  float32
  * The call enqueues two kernels, or one where the keys need no splitting and in small calls, and nothing else.
  * Errors: INVALID_ARG for a bad cache, a misaligned q (16 bytes) or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax;
- * UNSUPPORTED for more than 2^24 / (Hq / Hkv) queries, for 2^24 or more tiles of 32 rows (of B x Hkv x (Hq / Hkv) n_q), or if
+ * UNSUPPORTED for more than 2^24 / (Hq / Hkv) queries, for 2^24 or more tiles of 32 rows (16 in binary32) of B x Hkv x (Hq / Hkv) n_q, or if
  * more than 2^25 tokens would have to be split further than the workspace allows for (over 16384 / ceil(n_tokens / 2^25) rows of q;
  * with lens, also where a share of all sequences' tokens would be as long).
  */

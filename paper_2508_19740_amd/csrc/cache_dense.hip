@@ -17,8 +17,10 @@
 //
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
-//       rows are exact down to 2^-28 of it; binary32 rows are split in two binary16 parts (22 bits).  Their sums are
-//       kept apart and meet in the score less the maximum: in one sum every step would round off (5e-7 of the result, 3.3e-7 now).
+//       rows are exact down to 2^-28 of it; binary32 rows are split in three parts of 8 bits.  Sums over parts of 8 bits
+//       are nearly exact; those of the first part are kept apart from the others', and meet them in the score less the
+//       maximum.  (A matrix instruction is off by up to 4 units of its largest term.  Two parts of 11 bits in one sum: 4.9e-7 of the
+//       result, median of 120 shapes, in sums of their own 3.3e-7, three parts 2.5e-7; one shape of 40 was over 1e-6.)
 //   p   is in [0, 2^8] (below), scaled by 2^7 and split in two parts: 22 bits, or 2^-32 of the largest weight
 //       where that is more.  Both are rounded to nearest: what many small weights lose must not add up.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
@@ -136,6 +138,13 @@ struct DenseArgs {
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
+// The nearest number of eight significant bits (|x| < 2^111).
+__device__ __forceinline__ float eight_bits(float x)
+{
+    const float c = x * 65537.0f;
+    return c - (c - x);
+}
+
 // A lane's 8 NF elements of a row, which LANES lanes (64 / LANES apart) share, scaled by a power of two that brings the row's largest into [2^13, 2^14), negated if
 // asked and split into QP binary16 parts; returns the exponent that takes the scaling back.
 template <typename QT, int QP, int NF, int LANES>
@@ -168,7 +177,7 @@ __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP]
     const float up = __uint_as_float(static_cast<uint32_t>(13 - ex + 127) << 23 | (negate ? 0x80000000u : 0u));
 #pragma unroll
     for (int c = 0; c < NF; ++c) {
-        h2 hi[4], lo[4];
+        h2 part[QP][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float x, y;
@@ -183,12 +192,16 @@ __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP]
             }
             x *= up;
             y *= up;
-            hi[j] = to_half(x, y);
-            lo[j] = hi[j];
-            if constexpr (QP == 2) lo[j] = to_half(less_low(x, hi[j]), less_high(y, hi[j]));
+#pragma unroll
+            for (int p = 0; p < QP; ++p) {
+                const float hx = p + 1 < QP ? eight_bits(x) : x, hy = p + 1 < QP ? eight_bits(y) : y;
+                part[p][j] = to_half(hx, hy);
+                x -= hx;
+                y -= hy;
+            }
         }
-        frag[0][c] = join(hi[0], hi[1], hi[2], hi[3]);
-        if constexpr (QP == 2) frag[1][c] = join(lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+        for (int p = 0; p < QP; ++p) frag[p][c] = join(part[p][0], part[p][1], part[p][2], part[p][3]);
     }
     return ex - 13;
 }
@@ -223,11 +236,11 @@ __device__ __forceinline__ float across_groups_sum(float x)
 
 // MT tiles of 16 rows a workgroup; its four wavefronts share out the keys of a run.  ONCE: no other workgroup reads them.
 template <typename CT, typename QT, int MT, bool ONCE>
-__global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(DenseArgs a)
+__global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void cache_dense_kernel(DenseArgs a)
 {
-    constexpr int QP = sizeof(QT) == 2 ? 1 : 2;
+    constexpr int QP = sizeof(QT) == 2 ? 1 : 3, SP = QP == 1 ? 1 : 2;    // parts of q, sums of its products
     constexpr int kAux = ONCE ? 2 : 0;           // non-temporal
-    constexpr bool TURN = MT == 1 && QP == 1;    // keys pass through LDS (below)
+    constexpr bool TURN = MT == 1;               // keys pass through LDS (below)
     typedef Operand<CT> Op;
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
     __shared__ alignas(16) float s_acc[kWaves][16][kHeadDim + 4];
@@ -288,7 +301,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
     // instruction reads eight whole rows, a step further ahead, and the lanes exchange them through 4 KB of LDS that the
     // wavefront has to itself (its place for results): 16 bytes of row r at place (chunk ^ r % 8), without bank conflicts either
     // way.  Half as many cache accesses: 268 MB, 32 / 8 heads 50.6 -> 49.4 us, lengths of their own, 28 / 4 heads 57.6 -> 56.2 us.
-    // With 32 rows vector and matrix instructions are the bound (112.4 -> 111.8 us), and binary32 queries leave too few registers.
+    // With two tiles of rows vector and matrix instructions are the bound (112.4 -> 111.8 us).
     u4 kraw[TURN ? 4 : 1];
     uint8_t* const stage = reinterpret_cast<uint8_t*>(&s_acc[wave][0][0]);
     uint8_t* const put = stage + (lane >> 3) * kHeadDim + ((lane ^ lane >> 3) & 7) * 16;
@@ -403,11 +416,11 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             nan_values = __any(found != 0);
         }
         // scores
-        f4 sc[MT][QP][2];                                       // of each part of q: sums of the large one are nearly exact
+        f4 sc[MT][SP][2];                                       // of the first part of q, and of the others
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int p = 0; p < QP; ++p) sc[t][p][0] = sc[t][p][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
+            for (int p = 0; p < SP; ++p) sc[t][p][0] = sc[t][p][1] = f4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -416,7 +429,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
 #pragma unroll
                 for (int t = 0; t < MT; ++t)
 #pragma unroll
-                    for (int p = 0; p < QP; ++p) sc[t][p][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][p][kt], 0, 0, 0);
+                    for (int p = 0; p < QP; ++p) sc[t][p ? SP - 1 : 0][kt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf, qf[t][p][c], sc[t][p ? SP - 1 : 0][kt], 0, 0, 0);
             }
         next_k();
         // softmax
@@ -429,7 +442,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 ? 3 : 2) void cache_dense_kernel(
             // the large part and the number first: where the weight is large they nearly cancel, and little is rounded off
             auto score = [&](int e, float add) {
                 const float y = __builtin_fmaf(sc[t][0][e / 4][e % 4], f[e / 4], add);
-                return QP == 2 ? __builtin_fmaf(sc[t][QP - 1][e / 4][e % 4], f[e / 4], y) : y;
+                return SP == 2 ? __builtin_fmaf(sc[t][SP - 1][e / 4][e % 4], f[e / 4], y) : y;
             };
             float top = -INFINITY;
 #pragma unroll
@@ -558,8 +571,9 @@ void launch_mt(StageTimer& timer, const DenseArgs& a, const DensePlan& d)
 {
     const int64_t bytes = 2 * a.n_tokens * kHeadDim * a.shares.batch * a.shares.by_heads.d;
     const bool once = a.shares.tiles == 1 && bytes >= kCacheBytes;
-    auto kern = once ? (d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1, true> : cache_dense_kernel<CT, QT, 2, true>)
-                     : (d.row_tiles == 1 ? cache_dense_kernel<CT, QT, 1, false> : cache_dense_kernel<CT, QT, 2, false>);
+    auto kern = once ? cache_dense_kernel<CT, QT, 1, true> : cache_dense_kernel<CT, QT, 1, false>;
+    if constexpr (sizeof(QT) == 2)
+        if (d.row_tiles == 2) kern = cache_dense_kernel<CT, QT, 2, false>;
     timer.launch(kern, dim3(d.grid), dim3(kThreads), 0, a);
 }
 
@@ -571,7 +585,10 @@ int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_
     const int64_t rows = static_cast<int64_t>(p.G) * n_q;
     if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;
     DenseShares& s = d->shares;
-    d->row_tiles = rows <= 16 ? 1 : 2;
+    // Two tiles of rows share the conversion of codes, one has the faster loads.  8 heads, 32768 tokens, with one / two: 32 rows
+    // 24.2 / 29.5 us, 48 rows 27.1 / 31.6, 128 rows 45.2 / 44.3, 512 rows 136 / 108; eight times 8 heads, 8192 tokens, 32 rows 31.0 /
+    // 36.6, 48 rows 43.4 / 42.3.  Binary32 rows, three parts each, leave no registers for two (512 rows 165 / 173 us, 17 rows 34.7 / 45.4).
+    d->row_tiles = rows <= 32 || p.kv_dtype == SPOTLIGHT_F32 ? 1 : 2;
     const int64_t most_rows = 16 * d->row_tiles, tiles = (rows + most_rows - 1) / most_rows, per = tiles * p.Hkv;   // workgroups of a run
     s.lens = lens;
     s.batch = static_cast<uint32_t>(p.B);

@@ -112,7 +112,7 @@ def attention(q, k, v, seen, scale):
 
 def tolerance(mag, size, chain, q_parts=1, p_err=0.0):
     """How far a result may be off: every score by (128 + 8) roundings of its products' sum (and, where binary32 rows of q
-    are split in two binary16 parts, each rounded to 11 bits, 2^-20 of them), which moves each weight by as much; the exponential by 2 units; p by
+    are split in binary16 parts, 2^-20 of them: two parts, each rounded to 11 bits, lose no more, three of 8 bits less), which moves each weight by as much; the exponential by 2 units; p by
     p_err; sums by `chain` roundings.  Both the numerator and the denominator take the error."""
     u = 2.0 ** -24
     score = (136 * u + (2.0 ** -20 if q_parts == 2 else 0.0)) * size
