@@ -565,8 +565,8 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
 }
 
 // Codes that no other workgroup reads and no cache would hold until the next call: 268 MB, 32 / 8 heads 50.4 -> 45.3 us, with
-// lengths of their own, 28 / 4 heads 57.2 -> 52.3 us, 1074 MB 189 -> 162 us, with 32
-// rows 206 -> 183 us; but 134 MB, called again, 27.3 -> 29.4 us.
+// lengths of their own, 28 / 4 heads 57.2 -> 52.3 us, 1074 MB 189 -> 162 us,
+// with 32 rows 206 -> 183 us; but 134 MB, called again, 27.3 -> 29.4 us.
 template <typename CT, typename QT>
 void launch_mt(StageTimer& timer, const DenseArgs& a, const DensePlan& d)
 {
@@ -586,12 +586,13 @@ int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_
     const int64_t rows = static_cast<int64_t>(p.G) * n_q;
     if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;
     DenseShares& s = d->shares;
-    // Two tiles of rows share the reads of codes and their conversion, one has the faster loads.  With one / two, nothing in a cache,
-    // E4M3: 17 rows, 32 MB 20.1 / 21.5, 64 MB 27.0 / 30.7, 128 MB 39.5 / 38.3 us, 32 rows, 32 MB 20.9 / 25.4, 64 MB 27.9 / 33.4, 128 MB 39.2 /
-    // 40.6, 256 MB 66.3 / 60.6 (integers 71.9 / 62.7); 64 MB, 48 rows 27.1 / 31.6, 128 rows 45.2 / 44.3, 512 rows 136 / 108.
-    // Binary32 rows, three parts each, leave no registers for two (512 rows 165 / 173 us, 17 rows 34.7 / 45.4).
+    // Two tiles of rows share the reads of codes and their conversion, one has the faster loads.  With one / two, nothing in a
+    // cache, E4M3: 17 rows, 32 MB 20.1 / 21.5 us, 64 MB 27.0 / 30.7, 128 MB 39.5 / 38.3 (integers 39.6 / 37.9); 32 rows, 32 MB
+    // 20.9 / 25.4, 64 MB 27.9 / 33.4, 128 MB 39.2 / 40.6, 256 MB 66.3 / 60.6 (integers 71.9 / 62.7); 64 MB, 48 rows 27.1 / 31.6,
+    // 128 rows 45.2 / 44.3, 512 rows 136 / 108.  Binary32 rows, three parts each, leave no registers for two (512 rows 165 /
+    // 173 us, 17 rows 34.7 / 45.4).
     const int64_t bytes = 2 * n_tokens * kHeadDim * p.B * p.Hkv;
-    d->row_tiles = rows <= (bytes < kCacheBytes ? 32 : 16) || p.kv_dtype == SPOTLIGHT_F32 ? 1 : 2;
+    d->row_tiles = rows <= (bytes < kCacheBytes / 2 ? 32 : 16) || p.kv_dtype == SPOTLIGHT_F32 ? 1 : 2;
     const int64_t most_rows = 16 * d->row_tiles, tiles = (rows + most_rows - 1) / most_rows, per = tiles * p.Hkv;   // workgroups of a run
     s.lens = lens;
     s.batch = static_cast<uint32_t>(p.B);
