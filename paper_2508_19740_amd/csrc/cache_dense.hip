@@ -23,8 +23,13 @@
 //       result, median of 120 shapes, in sums of their own 3.3e-7, three parts 2.5e-7; one shape of 40 was over 1e-6.)
 //   p   is in [0, 2^8] (below), scaled by 2^7 and split in two parts: 22 bits, or 2^-32 of the largest weight
 //       where that is more.  Both are rounded to nearest: what many small weights lose must not add up.
-//   v   carries the ratio of its block's scale to the largest of the run's, times 2^5: exact where that
-//       ratio is above 2^-20, and at most 2^-30 of the largest block's size off below.
+//   v   carries the ratio of its block's scale to the largest of the run's, times 2^5, which is exact down to 2^-20.
+//
+// Where the scales of a run's values lie further apart than 2^12 (a key of huge values, or a block of zeros, whose scale
+// is the least there is), or one is NaN, a row must not lose the small values that it attends to a large one that it does not
+// see, or weighs 0.  There, the 16 keys of a block have products of their own (v_mfma_f32_16x16x16_f16), with weights relative to the row's
+// largest among them, and meet the others in binary32 with that weight and the block's scale: 64 more multiply-adds a tile.  (2^12: what the second part of p drops, 2^-32 of the largest weight, is then 2^-20 of the least
+// block's values at most.)
 //
 // A row reads 256 bytes a key and key-value head, whatever G and n_q: with few rows the kernel is bound by
 // memory.  The keys are split over workgroups, and a merge joins them.
@@ -37,6 +42,7 @@ using namespace cache;
 namespace {
 
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h4 __attribute__((ext_vector_type(4)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
@@ -45,6 +51,8 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = kDenseStep;       // keys of a step
 constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^7
 constexpr float kPUp = 7.0f;
+constexpr int kFar = 12;                // scales of values further apart than 2^12 have products of their own,
+constexpr int kApartUp = -20;           // summed times 2^-20: 2^12 values of the largest float's size stay finite
 constexpr float kSlack = 8.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
 constexpr int kInf = 0x7f800000;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -52,6 +60,12 @@ constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ h8 join(h2 a, h2 b, h2 c, h2 d)
 {
     return h8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// The elements of the first or the last 16 keys of a step.
+__device__ __forceinline__ h4 half_of(h8 x, int kt)
+{
+    return kt ? __builtin_shufflevector(x, x, 4, 5, 6, 7) : __builtin_shufflevector(x, x, 0, 1, 2, 3);
 }
 
 // Binary16 operands from codes.
@@ -351,12 +365,13 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
     const float* vs = a.v_scale + head * a.blocks;
     const uint32_t last_block = static_cast<uint32_t>(k0 + (n > 0 ? n - 1 : 0)) >> a.shift;   // tokens are below 2^31
 
-    // the largest scale of the run's values, as bits; NaN is left out
-    int unit_bits = 0;
+    // the largest scale of the run's values, as bits (NaN is more than infinity), and how far the least lies below infinity
+    int unit_bits = 0, low_bits = 0;
     if (n > 0)
         for (uint32_t j = (static_cast<uint32_t>(k0) >> a.shift) + lane; j <= last_block; j += 64) {
             const int v = reinterpret_cast<const int*>(vs)[j];
-            unit_bits = max(unit_bits, v > kInf ? 0 : v);
+            unit_bits = max(unit_bits, v);
+            low_bits = max(low_bits, kInf - v);
         }
     h8 qf[MT][QP][4];
     float factor[MT];
@@ -366,8 +381,10 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
         factor[t] = ldexpf(a.scale2, ex);
     }
     unit_bits = wave_max(unit_bits);
+    low_bits = wave_max(low_bits);
+    const bool apart = unit_bits > kInf || unit_bits - (kInf - low_bits) > kFar << 23;       // the same for the wavefront
     if (unit_bits == 0) unit_bits = 127 << 23;
-    const float to_value = ldexpf(__int_as_float(unit_bits), -kVUp);
+    const float to_value = apart ? ldexpf(1.0f, -kApartUp) : ldexpf(__int_as_float(unit_bits), -kVUp);
     unit_bits -= (127 + kVUp) << 23;
 
     f4 acc[MT][8];
@@ -393,28 +410,25 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
     if (steps > 0) load_scales(0);
     if constexpr (TURN) next_k();
 
-    auto step = [&](int s, auto masked) {
+    // alone: the blocks' values have products of their own
+    auto step = [&](int s, auto masked, auto alone) {
+        constexpr bool ALONE = decltype(alone)::value;
         // the scales of this step; the next one's are on their way from here on
-        float kscale[2];
+        float kscale[2], vscale[2];
         typename Op::Ratio ratio[2];
-        bool nan_values = false;                                // of this step; asked only where a row sees part of it
+        bool nan_block[2] = {false, false};
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             kscale[t] = next_ks[t];
-            const int v = next_vs[t], up = v - unit_bits;       // powers of two: a difference of exponents
-            const bool nan = v > kInf;
-            ratio[t] = Op::ratio(__int_as_float(nan ? v : up > 0 ? up : 0));
-            if constexpr (decltype(masked)::value && !CT::kHasNaN) nan_values |= nan;
+            if constexpr (ALONE) {
+                nan_block[t] = next_vs[t] > kInf;
+                vscale[t] = nan_block[t] ? 0.0f : __int_as_float(next_vs[t]);
+                ratio[t] = Op::ratio(1.0f);
+            } else {
+                ratio[t] = Op::ratio(__int_as_float(next_vs[t] - unit_bits));   // powers of two: a difference of exponents
+            }
         }
         load_scales(s + 1);
-        if constexpr (decltype(masked)::value && CT::kHasNaN) {
-            uint32_t found = 0;                                 // bytes of 7f and ff
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) found |= (((vreg[t][r].x & 0x7f7f7f7fu) + 0x01010101u) | ((vreg[t][r].y & 0x7f7f7f7fu) + 0x01010101u)) & 0x80808080u;
-            nan_values = __any(found != 0);
-        }
         // scores
         f4 sc[MT][SP][2];                                       // of the first part of q, and of the others
 #pragma unroll
@@ -434,6 +448,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
         next_k();
         // softmax
         h8 hi[MT], lo[MT];
+        float back[MT][2];                                      // takes a block's products to the sum's unit
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             float f[2], x[8];
@@ -452,7 +467,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
                     if (s * kStep + 16 * (e / 4) + 4 * g + e % 4 >= sees[t]) x[e] = -INFINITY;
                 top = fmaxf(top, x[e]);
             }
-            if (__any(!(top <= kPUp + kSlack))) {          // also before the first maximum
+            if (__any(!(top <= (ALONE ? kPUp : kPUp + kSlack)))) {   // also before the first maximum
                 float high = -INFINITY;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -473,9 +488,25 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = x[e] > -INFINITY ? x[e] + base[t] : x[e];
             }
+            float up[2] = {0.0f, 0.0f};                     // what the weights in the products are scaled by, log2
+            if constexpr (ALONE) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(x[e]);
-            l[t] += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+                for (int kt = 0; kt < 2; ++kt) {
+                    float most = -400.0f;                       // less weighs 0 whatever its value
+#pragma unroll
+                    for (int e = 4 * kt; e < 4 * kt + 4; ++e) most = fmaxf(most, x[e]);
+                    most = ceilf(across_groups_max(most));
+                    up[kt] = kPUp - most;
+                    back[t][kt] = ldexpf(vscale[kt], static_cast<int>(-up[kt]) + kApartUp);
+                }
+            }
+            float w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                w[e] = __builtin_amdgcn_exp2f(x[e]);
+                x[e] = ALONE ? __builtin_amdgcn_exp2f(x[e] + up[e / 4]) : w[e];
+            }
+            l[t] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
             h2 h[4], r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -485,6 +516,47 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
             hi[t] = join(h[0], h[1], h[2], h[3]);
             lo[t] = join(r[0], r[1], r[2], r[3]);
         }
+        // A row's weight 0 must not meet a NaN of a key that it does not see: the products are formed without NaN, and the
+        // sums of the rows that see one become NaN.
+        if constexpr (ALONE) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                if ((nan_block[0] && s * kStep < sees[t]) || (nan_block[1] && s * kStep + 16 < sees[t]))
+#pragma unroll
+                    for (int d = 0; d < 8; ++d) acc[t][d] += __builtin_nanf("");
+        }
+        if constexpr (decltype(masked)::value && CT::kHasNaN) {
+            auto nan_bytes = [](uint32_t v) { return ((v & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; };      // 7f and ff
+            uint32_t any = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) any |= nan_bytes(vreg[e / 4][e % 4].x) | nan_bytes(vreg[e / 4][e % 4].y);
+            if (__any(any != 0)) {
+                h8 sees_key[MT];
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sees_key[t][j] = s * kStep + 16 * (j / 4) + 4 * g + j % 4 < sees[t] ? 1.0f16 : 0.0f16;
+#pragma unroll
+                for (int d = 0; d < 8; ++d) {
+                    h8 is_nan;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) is_nan[j] = (vreg[j / 4][j % 4][d / 4] >> (8 * (d % 4)) & 0x7fu) == 0x7fu ? 1.0f16 : 0.0f16;
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        const f4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is_nan, sees_key[t], f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (hit[r] != 0.0f) acc[t][d][r] = __builtin_nanf("");
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    u2& v = vreg[e / 4][e % 4];
+                    v = u2{v.x & ~((nan_bytes(v.x) >> 7) * 0xffu), v.y & ~((nan_bytes(v.y) >> 7) * 0xffu)};
+                }
+            }
+        }
         // weighted values: four columns of the lane at a time
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
@@ -493,42 +565,32 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
             for (int pr = 0; pr < 4; ++pr) Op::columns(vreg[pr / 2][2 * (pr % 2)][w], vreg[pr / 2][2 * (pr % 2) + 1][w], ratio[pr / 2], col[pr]);
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                h8 vf = join(col[0][c], col[1][c], col[2][c], col[3][c]);
-                if constexpr (decltype(masked)::value) {
-                    // A row's weight 0 must not meet a NaN of a key that it does not see: the product is
-                    // formed without NaN, and one of "is NaN" and "sees the key" tells which sums are NaN.
-                    if (nan_values) {
-                        h8 is_nan;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const bool bad = !(vf[j] == vf[j]);
-                            is_nan[j] = bad ? 1.0f16 : 0.0f16;
-                            vf[j] = bad ? 0.0f16 : vf[j];
-                        }
-#pragma unroll
-                        for (int t = 0; t < MT; ++t) {
-                            h8 sees_key;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) sees_key[j] = s * kStep + 16 * (j / 4) + 4 * g + j % 4 < sees[t] ? 1.0f16 : 0.0f16;
-                            const f4 hit = __builtin_amdgcn_mfma_f32_16x16x32_f16(is_nan, sees_key, f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
-#pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (hit[r] != 0.0f) acc[t][4 * w + c][r] = __builtin_nanf("");
-                        }
-                    }
-                }
+                const h8 vf = join(col[0][c], col[1][c], col[2][c], col[3][c]);
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[t], acc[t][4 * w + c], 0, 0, 0);
-                    acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[t], acc[t][4 * w + c], 0, 0, 0);
+                    if constexpr (ALONE) {
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) {
+                            f4 sum = __builtin_amdgcn_mfma_f32_16x16x16f16(half_of(vf, kt), half_of(hi[t], kt), f4{0.0f, 0.0f, 0.0f, 0.0f}, 0, 0, 0);
+                            sum = __builtin_amdgcn_mfma_f32_16x16x16f16(half_of(vf, kt), half_of(lo[t], kt), sum, 0, 0, 0);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc[t][4 * w + c][r] = __builtin_fmaf(sum[r], back[t][kt], acc[t][4 * w + c][r]);
+                        }
+                    } else {
+                        acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, hi[t], acc[t][4 * w + c], 0, 0, 0);
+                        acc[t][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, lo[t], acc[t][4 * w + c], 0, 0, 0);
+                    }
                 }
+                if constexpr (ALONE) __builtin_amdgcn_sched_barrier(0);      // a column at a time: no registers for more
             }
         }
         load_v();
     };
     int s = 0;
-    for (; s < plain_steps; ++s) step(s, Flag<false>{});
-    for (; s < steps; ++s) step(s, Flag<true>{});
+    if (apart)
+        for (; s < steps; ++s) step(s, Flag<true>{}, Flag<true>{});
+    for (; s < plain_steps; ++s) step(s, Flag<false>{}, Flag<false>{});
+    for (; s < steps; ++s) step(s, Flag<true>{}, Flag<false>{});
 
     // the wavefronts' results, joined: lane (g, i) has columns 32g .. 32g+31 of row i
 #pragma unroll
