@@ -51,8 +51,10 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 constexpr int kStep = kDenseStep;       // keys of a step
 constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^7
 constexpr float kPUp = 7.0f;
-constexpr int kFar = 12;                // scales of values further apart than 2^12 have products of their own,
-constexpr int kApartUp = -20;           // summed times 2^-20: 2^12 values of the largest float's size stay finite
+constexpr int kFar = 12;                // scales of values further apart than 2^12 have products of their own
+// Partial results are sums of weights and of weighted values, the largest weight 2^7 to 2^15, times 2^-20: of values of
+// the largest float's size, 2^13 with all the same weight add up without an overflow; and values are whole down to 2^-113.
+constexpr int kSumUp = -20;
 constexpr float kSlack = 8.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
 constexpr int kInf = 0x7f800000;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
     low_bits = wave_max(low_bits);
     const bool apart = unit_bits > kInf || unit_bits - (kInf - low_bits) > kFar << 23;       // the same for the wavefront
     if (unit_bits == 0) unit_bits = 127 << 23;
-    const float to_value = apart ? ldexpf(1.0f, -kApartUp) : ldexpf(__int_as_float(unit_bits), -kVUp);
+    const int to_sum = apart ? 0 : (unit_bits >> 23) - 127 - kVUp + kSumUp;                  // from the products' unit, log2
     unit_bits -= (127 + kVUp) << 23;
 
     f4 acc[MT][8];
@@ -497,7 +499,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
                     for (int e = 4 * kt; e < 4 * kt + 4; ++e) most = fmaxf(most, x[e]);
                     most = ceilf(across_groups_max(most));
                     up[kt] = kPUp - most;
-                    back[t][kt] = ldexpf(vscale[kt], static_cast<int>(-up[kt]) + kApartUp);
+                    back[t][kt] = ldexpf(vscale[kt], static_cast<int>(-up[kt]) + kSumUp);
                 }
             }
             float w[8];
@@ -597,13 +599,13 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
     for (int t = 0; t < MT; ++t) {
         const float sum = across_groups_sum(l[t]);
         if (t) __syncthreads();
-        if (g == 0) { s_m[wave][i] = kPUp - base[t]; s_l[wave][i] = sum; }
+        if (g == 0) { s_m[wave][i] = kPUp - base[t]; s_l[wave][i] = ldexpf(sum, kSumUp); }
 #pragma unroll
         for (int r = 0; r < 4; ++r)
 #pragma unroll
             for (int d = 0; d < 8; d += 4)
                 *reinterpret_cast<f4*>(&s_acc[wave][i][g * 32 + r * 8 + d]) =
-                    f4{acc[t][d][r], acc[t][d + 1][r], acc[t][d + 2][r], acc[t][d + 3][r]} * to_value;
+                    f4{ldexpf(acc[t][d][r], to_sum), ldexpf(acc[t][d + 1][r], to_sum), ldexpf(acc[t][d + 2][r], to_sum), ldexpf(acc[t][d + 3][r], to_sum)};
         __syncthreads();
         const int left = static_cast<int>(a.rows - min(r0 + 16 * t, a.rows));
         for (int e = tid; e < 16 * 64 && e / 64 < left; e += kThreads) {

@@ -167,3 +167,43 @@ def test_nan_scales(nq, n, block, code, kv):
                 clean &= ~one
             _check(out[0, h, clean], want[clean], tol[clean], (which, beside, h))
         ctx.close()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("nq,n,block", [(1, 1, 16), (1, 2, 16), (1, 70, 32), (1, 4000, 64), (1, 8192, 128), (3, 3, 16), (20, 700, 16), (70, 300, 64)])
+def test_values_near_the_largest_and_the_smallest(nq, n, block, code, kv):
+    """Values up to the largest float's size, and down to 2^-110: weighted means of them are of their size, whatever sums are
+    formed on the way.  (Scores are small: no key takes all the weight.)"""
+    for size in (120, 127, -110):
+        host = cc.random_cache(1, 1, n, block, code, 7, spread=0.0)
+        top = 8 if code == "e4m3" else 6
+        host.scale["v"][:] = 2.0 ** (size - top)
+        host.codes["v"] = cc.nearest(torch.rand(1, 1, n, cc.D, generator=torch.Generator().manual_seed(n), dtype=torch.float64) * 1.75 * 2 ** top, code)
+        ctx = _ctx(2, 1, n, kv)
+        q = _q(4, kv, 1, 2, nq, size=0.5)
+        out = ctx.dense_decode_cache(q.to(DEV), host.device(), n)
+        for h in range(2):
+            want, tol = _want(q[0, h], host, 0, n, nq)
+            _check(out[0, h], want, tol - 1e-37 + 2.0 ** -135, (size, h))
+        ctx.close()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "i8"])
+@pytest.mark.parametrize("n,block", [(600, 32), (5000, 64)])
+def test_the_largest_values_with_no_weight(n, block, code):
+    """Keys of the largest values there are, a whole block of them, that weigh nothing."""
+    host = cc.random_cache(1, 1, n, block, code, 5)
+    blk = n // 2 // block
+    rows = slice(blk * block, (blk + 1) * block)
+    host.codes["v"][0, 0, rows] = cc.MOST[code]
+    host.scale["v"][0, 0, blk] = 2.0 ** (119 if code == "e4m3" else 121)
+    q = _q(4, "bf16", 1, 1, 1)
+    c = 400.0 / float(q.double().abs().sum() * SCALE)
+    host.scale["k"][0, 0, blk] = cc.least_scale(c, code)
+    host.codes["k"][0, 0, rows] = cc.nearest(-torch.sign(q[0, 0, 0].double()) * c / host.scale["k"][0, 0, blk], code)
+    ctx = _ctx(1, 1, n)
+    out = ctx.dense_decode_cache(q.to(DEV), host.device(), n)
+    want, tol = _want(q[0, 0], host, 0, n, 1)
+    _check(out[0, 0], want, tol, n)
+    ctx.close()
