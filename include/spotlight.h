@@ -18,7 +18,7 @@
  *   - Return value: SPOTLIGHT_OK (0) or a negative SPOTLIGHT_ERR_* code.  Arguments are checked
  *     on the host before the first HIP call, so argument errors never touch the GPU.
  *   - One context must not be used from two threads at once; calls that overlap on one context
- *     share its workspace and race.
+ *     share its workspace and race: their results are undefined, those of later calls are not.
  *
  * Symbols: d = head_dim (128), B = batch, Hq / Hkv = query / key-value heads, G = Hq / Hkv,
  * L = code_bits, W = L / 32, h = hidden, Nmax = max_tokens.  Query head hq reads key-value head
@@ -119,7 +119,7 @@ size_t spotlight_workspace_bytes(const spotlight_config *cfg);
  * lists (about one byte per (query head, token)), the partial attention results, a bit per key and
  * norms of the hash weights for bulk hashing (a second copy of bfloat16 weights that do not fit into
  * LDS), room for one copy of the hash weights (spotlight_prepack_weights), and for the partial results of
- * attention over the whole of an 8-bit cache (8.1 MiB, less for short caches, more from 8193 query heads on; they lie
+ * attention over the whole of an 8-bit cache (8.3 MiB, less for short caches, more from 8193 query heads on; they lie
  * over retrieval's scratch memory where that is large enough). */
 int spotlight_create(spotlight_ctx **out, const spotlight_config *cfg);
 

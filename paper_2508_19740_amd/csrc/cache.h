@@ -65,6 +65,21 @@ inline bool joins_in_place(int64_t workgroups, int64_t rows, int64_t nsplit)
     return nsplit > 1 && rounds <= 1 && workgroups <= kJoinGroups;
 }
 
+// The counter of the at-th group of rows among those of a call that have nsplit parts (2 .. kJoinSplits; at < kJoinGroups /
+// nsplit).  A counter belongs to one nsplit for good and wraps there, so that it is 0 again after any number of calls, also
+// where a program lets calls overlap, whose results are then undefined: the next call's are not.  (A counter that the last
+// workgroup clears would lose or keep counts then, and no workgroup of later calls would be the last.)
+constexpr
+#if defined(__HIPCC__)
+__host__ __device__
+#endif
+uint32_t arrival_counter(uint32_t at, uint32_t nsplit)
+{
+    const uint32_t k = 31 - __builtin_clz(nsplit);
+    return (k - 1) * kJoinGroups + (nsplit - (1u << k)) * (kJoinGroups >> k) + at;
+}
+static_assert(arrival_counter(0, 2) == 0 && arrival_counter(kJoinGroups / kJoinSplits - 1, kJoinSplits) < kArrivedCounters, "counters");
+
 // The rows that the merge kernel joins: nsplit partial results each, one after the other; or (runs set) those of attention
 // over the whole cache, where the runs of a sequence lie apart.
 struct MergeRows {
@@ -137,11 +152,11 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float(st
 // Its reads have to see what workgroups on other dies wrote: there, partial results are written and read with
 // device-wide (relaxed atomic) accesses, which no die's cache holds back, and every wavefront waits for its writes
 // before its workgroup counts itself as arrived.  (A release fence would write back all of the die's cache instead, once
-// a workgroup.)  A counter is 0 between calls.
+// a workgroup.)
 struct Partials {
     unsigned long long* ml;             // [rows][nsplit] float2
     unsigned long long* acc;            // [rows][nsplit][64] float2
-    uint32_t* arrived;                  // of each group of rows, kArrivedStride apart; null: another kernel joins
+    uint32_t* arrived;                  // the counters, kArrivedStride apart; null: another kernel joins
 };
 
 __device__ __forceinline__ void put_pair(unsigned long long* p, float x, float y)
@@ -165,16 +180,12 @@ __device__ __forceinline__ void put_part(const Partials& p, size_t at, uint32_t 
     }
 }
 
-// Counts the workgroup as arrived once its writes are done; true for the last of them.
-__device__ __forceinline__ bool arrives_last(uint32_t* arrived, uint32_t nsplit, uint32_t* lds)
+// Counts the workgroup as arrived once its writes are done; true for the last of the group's (arrival_counter).
+__device__ __forceinline__ bool arrives_last(const Partials& p, uint32_t at, uint32_t nsplit, uint32_t* lds)
 {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (threadIdx.x == 0) {
-        const uint32_t before = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (before == nsplit - 1) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *lds = before;
-    }
+    if (threadIdx.x == 0) *lds = atomicInc(p.arrived + arrival_counter(at, nsplit) * kArrivedStride, nsplit - 1);
     __syncthreads();
     asm volatile("" ::: "memory");
     return *lds == nsplit - 1;

@@ -223,7 +223,7 @@ __global__ __launch_bounds__(NT) void cache_attend_kernel(AttendArgs a)
     }
     if constexpr (JOINS) {
         if (!a.part.arrived) return;
-        if (arrives_last(a.part.arrived + bh * kArrivedStride, static_cast<uint32_t>(a.nsplit), &s_before))
+        if (arrives_last(a.part, static_cast<uint32_t>(bh), static_cast<uint32_t>(a.nsplit), &s_before))
             join_rows<NT, 16>(a.part, static_cast<uint32_t>(bh) * a.nsplit, 1, 1, static_cast<uint32_t>(a.nsplit), a.out + bh * kHeadDim, reinterpret_cast<f32x2*>(&s_acc[0][0]));
     }
 }

@@ -18,9 +18,11 @@ constexpr int kAttendMinRows = 32;  // smallest number of gathered rows one work
 constexpr int kTokensPerBlock = 4096;  // tokens one score / select workgroup covers
 constexpr int kCandCap = 1024;      // candidate-list entries per (query head, token block)
 constexpr int kMaxProfile = 8192;
-constexpr int kJoinGroups = 256;    // groups of rows whose partial results their last workgroup joins, at most
-constexpr int kArrivedStride = 32;  // words between their counters: atomics on one line wait for each other
-constexpr size_t kArrivedBytes = static_cast<size_t>(kJoinGroups) * kArrivedStride * 4;
+constexpr int kJoinGroups = 256;    // workgroups of a call whose partial results the last of each group of rows joins, at most,
+constexpr int kJoinSplits = 64;     // and of such a group
+constexpr int kArrivedStride = 32;  // words between the groups' counters: atomics on one line wait for each other
+constexpr int kArrivedCounters = 6 * kJoinGroups;   // as many for each power of two that a group's size may begin with
+constexpr size_t kArrivedBytes = static_cast<size_t>(kArrivedCounters) * kArrivedStride * 4;
 
 // Geometry derived once from the configuration.
 struct Plan {
@@ -51,7 +53,7 @@ struct Plan {
     size_t off_dense_acc;  // [dense_rows][128] weighted value sums of each split
     int64_t dense_rows;
     size_t off_runs;       // [B] {first run, runs} of each sequence in that attention
-    size_t off_arrived;    // [kArrivedBytes] workgroups of each group of rows that have written their part; 0 between calls
+    size_t off_arrived;    // [kArrivedBytes] workgroups of each group of rows that have written their part; 0 between calls (cache.h)
     size_t off_audit;      // AuditRec of the bulk hash (SPOTLIGHT_OPT_BULK_HASH_AUDIT)
     size_t total_bytes;
 };
