@@ -88,7 +88,24 @@ struct MergeRows {
     const uint2* runs;          // [batch] {first, number}
     FastDiv by_rows, by_heads, by_tile;
     uint32_t tiles, tile_rows;
+    int64_t room;               // partial results that the workspace holds
 };
+
+// Where the partial results of a row lie: nsplit of them, `step` apart.  The table of runs is read from the workspace.  Where a
+// program lets calls overlap, it may be another call's, with more runs than this call's tiles leave room for: those are left out.
+struct RowParts { int64_t at, step; int nsplit; };
+#if defined(__HIPCC__)
+__host__ __device__
+#endif
+inline RowParts parts_of(const MergeRows& r, uint2 run, uint32_t kv, uint32_t tile, uint32_t row)
+{
+    RowParts p;
+    p.step = static_cast<int64_t>(r.by_heads.d) * r.tiles * r.tile_rows;
+    p.at = ((static_cast<int64_t>(run.x) * r.by_heads.d + kv) * r.tiles + tile) * r.tile_rows + row;
+    p.nsplit = static_cast<int>(run.y);
+    if (p.at + (p.nsplit - 1) * p.step >= r.room) p.nsplit = 0;
+    return p;
+}
 
 #if defined(__HIPCC__)
 

@@ -253,7 +253,7 @@ int launch_t(spotlight_ctx* ctx, AttendArgs& a)
         if (hipGetLastError() != hipSuccess) return SPOTLIGHT_ERR_HIP;
     }
     if (a.nsplit == 1 || a.part.arrived) return SPOTLIGHT_OK;
-    return launch_cache_merge(ctx, a.part.ml, a.part.acc, MergeRows{heads, a.nsplit, nullptr, {}, {}, {}, 0, 0}, a.nsplit, a.out);
+    return launch_cache_merge(ctx, a.part.ml, a.part.acc, MergeRows{heads, a.nsplit, nullptr, {}, {}, {}, 0, 0, 0}, a.nsplit, a.out);
 }
 
 }  // namespace

@@ -756,7 +756,7 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     }
     if (done) return SPOTLIGHT_OK;
     const MergeRows r{static_cast<int64_t>(p.B) * p.Hkv * a.rows, 0, a.runs, fast_div(a.rows), fast_div(static_cast<uint32_t>(p.Hkv)),
-                      fast_div(16u * d.row_tiles), d.shares.tiles, d.shares.tile_rows};
+                      fast_div(16u * d.row_tiles), d.shares.tiles, d.shares.tile_rows, p.dense_rows};
     return launch_cache_merge(ctx, a.part.ml, a.part.acc, r, d.about, out);
 }
 

@@ -24,11 +24,10 @@ __global__ __launch_bounds__(kThreads) void cache_merge_kernel(const float2* __r
     if (r.runs) {
         const uint32_t head = r.by_rows.over(static_cast<uint32_t>(have)), in_head = static_cast<uint32_t>(have) - head * r.by_rows.d;
         const uint32_t entry = r.by_heads.over(head), tile = r.by_tile.over(in_head);
-        const uint2 run = r.runs[entry];
-        nsplit = static_cast<int>(run.y);
-        at = (static_cast<int64_t>(run.x) * r.by_heads.d + (head - entry * r.by_heads.d)) * r.tiles + tile;
-        at = at * r.tile_rows + (in_head - tile * r.by_tile.d);
-        step = static_cast<int64_t>(r.by_heads.d) * r.tiles * r.tile_rows;
+        const RowParts p = parts_of(r, r.runs[entry], head - entry * r.by_heads.d, tile, in_head - tile * r.by_tile.d);
+        at = p.at;
+        step = p.step;
+        nsplit = p.nsplit;
     }
     float m = -INFINITY, l = 0.0f;
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);

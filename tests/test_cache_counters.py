@@ -1,5 +1,7 @@
-"""The counters by which the last workgroup of a group of rows is found (attention over the 8-bit cache, small calls), without a GPU:
-each group of a call has one of its own, and calls that a program lets overlap leave nothing behind for later ones."""
+"""What the kernels of attention over the 8-bit cache keep in the workspace, without a GPU.  The counters by which the last workgroup of
+a group of rows is found (small calls): each group of a call has one of its own, and calls that a program lets overlap leave
+nothing behind for later ones.  The table of runs by which partial results are merged: all that a call's own table names lies in the
+workspace, and so does what is read by the table of another call."""
 import os
 import subprocess
 
@@ -141,16 +143,65 @@ int main(int argc, char** argv)
 """
 
 
-@pytest.fixture(scope="module")
-def program(tmp_path_factory):
-    src = tmp_path_factory.mktemp("counters") / "host.cpp"
+TABLES = HEAD + r"""
+#include <random>
+#include <vector>
+int main()
+{
+    std::mt19937 rng(3);
+    long merged = 0, refused = 0;
+    for (int B : {1, 3, 16, 100})
+        for (int Hkv : {1, 4, 8})
+            for (int G : {1, 4, 7})
+                for (long n : {300L, 5000L, 131072L, 1L << 25}) {
+                    const spotlight_config cfg = config(B, Hkv * G, Hkv, n, 1);
+                    Plan p;
+                    if (make_plan(&cfg, &p) != SPOTLIGHT_OK) return 2;
+                    std::vector<cache::DensePlan> plans;
+                    for (int nq : {1, 2, 17, 128, 300})
+                        for (int ragged : {0, 1}) {
+                            cache::DensePlan d;
+                            int32_t one;
+                            if (cache::plan_dense(p, 256, n, nq, ragged ? &one : nullptr, &d) == SPOTLIGHT_OK && d.splits) plans.push_back(d);
+                        }
+                    for (const auto& mine : plans)
+                        for (const auto& table : plans) {
+                            cache::MergeRows r = {};
+                            r.by_heads = cache::fast_div(Hkv);
+                            r.tiles = mine.shares.tiles;
+                            r.tile_rows = mine.shares.tile_rows;
+                            r.room = p.dense_rows;
+                            const uint32_t most = table.shares.most_runs ? table.shares.most_runs : table.shares.nsplit * B;
+                            for (int k = 0; k < 20; ++k) {
+                                const uint32_t number = k == 0 ? std::min(most, table.shares.nsplit) : 1 + rng() % std::min(most, table.shares.nsplit);
+                                const uint2 run = {k == 1 ? 0 : k == 0 ? most - number : static_cast<uint32_t>(rng() % (most - number + 1)), number};
+                                const cache::RowParts x = cache::parts_of(r, run, Hkv - 1, r.tiles - 1, r.tile_rows - 1);
+                                const long last = x.at + (x.nsplit - 1) * x.step;
+                                if (&mine == &table && x.nsplit != static_cast<int>(number)) return 3;      // its own: all of it
+                                if (x.nsplit != 0 && (x.at < 0 || last >= p.dense_rows)) return 4;
+                                (x.nsplit ? merged : refused) += 1;
+                            }
+                        }
+                }
+    return merged > 1000 && refused > 1000 ? 0 : 5;
+}
+"""
+
+
+def _build(folder, source):
+    src = folder / "host.cpp"
     exe = str(src)[:-4]
-    src.write_text(COUNTERS)
+    src.write_text(source)
     lib = sp.lib._name
     subprocess.run(["g++", "-std=c++17", "-O1", "-D__HIP_PLATFORM_AMD__", "-w", "-I", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"),
                     "-I", CSRC, str(src), "-o", exe, lib, f"-Wl,-rpath,{os.path.dirname(lib)}", "-L/opt/rocm/lib",
                     "-lamdhip64", "-Wl,-rpath,/opt/rocm/lib"], check=True)
     return exe
+
+
+@pytest.fixture(scope="module")
+def program(tmp_path_factory):
+    return _build(tmp_path_factory.mktemp("counters"), COUNTERS)
 
 
 def test_counters_recover(program):
@@ -162,3 +213,8 @@ def test_the_model_sees_counters_that_do_not(program):
     """With one counter for groups of any size, cleared by the last, overlapping calls leave a later call without its last."""
     run = subprocess.run([program, "cleared"], capture_output=True, text=True)
     assert run.returncode == 4, run.stdout
+
+
+def test_the_merge_stays_in_the_workspace(tmp_path):
+    run = subprocess.run([_build(tmp_path, TABLES)], capture_output=True, text=True)
+    assert run.returncode == 0, run.returncode
