@@ -6,8 +6,8 @@
 //   S^T = K Q^T     v_mfma_f32_16x16x32_f16.  Lane (g, i) = (lane / 16, lane % 16) loads 32 adjacent
 //                   bytes of key i; four products take 8 of them each, and q lies in registers in the
 //                   same order.  The result leaves lane (g, i) with keys 4g .. 4g+3 of query row i.
-//   softmax         weights are relative to a maximum that was taken once.  Lanes compare their own scores
-//                   with it, and only where one is more than 8 (a factor of 2^8) above it is the maximum taken
+//   softmax         weights are relative to a maximum that was taken once, rounded up to a whole number (of log2).  Lanes compare
+//                   their own scores with it, and only where one is more than 7 (a factor of 2^7) above it is the maximum taken
 //                   anew, over the lanes, and what has been summed rescaled.  (Taken at every larger score, some row
 //                   of 16 had one at most steps; at 4 above, at one step in three.)
 //   O^T += V^T P^T  The lane holds the weights just where the second operand wants them (the keys of a
@@ -17,11 +17,13 @@
 //
 // Both codes are exact in binary16, so the products' only rounding is that of their binary32 sums:
 //   q   is scaled by a power of two for each row to a largest magnitude in [2^13, 2^14), where bfloat16
-//       rows are exact down to 2^-28 of it; binary32 rows are split in three parts of 8 bits.  Sums over parts of 8 bits
-//       are nearly exact; those of the first part are kept apart from the others', and meet them in the score less the
-//       maximum.  (A matrix instruction is off by up to 4 units of its largest term.  Two parts of 11 bits in one sum: 4.9e-7 of the
-//       result, median of 120 shapes, in sums of their own 3.3e-7, three parts 2.5e-7; one shape of 40 was over 1e-6.)
-//   p   is in [0, 2^8] (below), scaled by 2^7 and split in two parts: 22 bits, or 2^-32 of the largest weight
+//       rows are exact down to 2^-28 of it; binary32 rows are split in three parts, multiples of 2^6, of 2^-2, and the rest,
+//       which is off by 2^-28 of the row's largest at most.  A matrix instruction is off by up to 4 units of its largest
+//       term; but sums of the first part by integer codes are below 2^24 of its units, and exact.  They are kept apart from the
+//       others' (2^-8 of them), and meet them in the score less the maximum.  (Error of the result, median of 40 seeds each of 6
+//       shapes: 1.7e-7 to 2.3e-7, with parts of eight significant bits of each element 2.0e-7 to 2.7e-7, of torch operations in
+//       binary32 4.9e-7 to 9.0e-7; of a single row of 4096 keys 9e-7 at most, theirs 1.7e-6, but less in 12 of 80.)
+//   p   is scaled to a largest of 2^7 to 2^15 (below) and split in two parts: 22 bits, or 2^-32 of the largest weight
 //       where that is more.  Both are rounded to nearest: what many small weights lose must not add up.
 //   v   carries the ratio of its block's scale to the largest of the run's, times 2^5, which is exact down to 2^-20.
 //
@@ -49,13 +51,13 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = kDenseStep;       // keys of a step
-constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^7
-constexpr float kPUp = 7.0f;
+constexpr int kVUp = 5;                 // v is scaled by 2^5, p by 2^8 less the maximum rounded up
+constexpr float kPUp = 8.0f;
 constexpr int kFar = 12;                // scales of values further apart than 2^12 have products of their own
 // Partial results are sums of weights and of weighted values, the largest weight 2^7 to 2^15, times 2^-20: of values of
 // the largest float's size, 2^13 with all the same weight add up without an overflow; and values are whole down to 2^-113.
 constexpr int kSumUp = -20;
-constexpr float kSlack = 8.0f;          // by which scores may pass the last maximum (log2) before it is taken anew
+constexpr float kSlack = 7.0f;          // by which scores may pass the last maximum (log2, rounded up) before it is taken anew
 constexpr int kInf = 0x7f800000;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -154,15 +156,15 @@ struct DenseArgs {
 
 template <bool B> struct Flag { static constexpr bool value = B; };
 
-// The nearest number of eight significant bits (|x| < 2^111).
-__device__ __forceinline__ float eight_bits(float x)
+// The nearest multiple of a power of two (|x| below 2^22 of them).
+__device__ __forceinline__ float multiple_of(float unit, float x)
 {
-    const float c = x * 65537.0f;
-    return c - (c - x);
+    const float c = 0x1.8p23f * unit;
+    return (x + c) - c;
 }
 
 // A lane's 8 NF elements of a row, which LANES lanes (64 / LANES apart) share, scaled by a power of two that brings the row's largest into [2^13, 2^14), negated if
-// asked and split into QP binary16 parts; returns the exponent that takes the scaling back.
+// asked and split into QP binary16 parts (multiples of 2^6, of 2^-2, and the rest); returns the exponent that takes the scaling back.
 template <typename QT, int QP, int NF, int LANES>
 __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP][NF])
 {
@@ -210,7 +212,7 @@ __device__ __forceinline__ int load_row(const QT* q, bool negate, h8 (&frag)[QP]
             y *= up;
 #pragma unroll
             for (int p = 0; p < QP; ++p) {
-                const float hx = p + 1 < QP ? eight_bits(x) : x, hy = p + 1 < QP ? eight_bits(y) : y;
+                const float unit = p == 0 ? 0x1p6f : 0x1p-2f, hx = p + 1 < QP ? multiple_of(unit, x) : x, hy = p + 1 < QP ? multiple_of(unit, y) : y;
                 part[p][j] = to_half(hx, hy);
                 x -= hx;
                 y -= hy;
@@ -390,7 +392,9 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
     unit_bits -= (127 + kVUp) << 23;
 
     f4 acc[MT][8];
-    float base[MT], l[MT];                       // kPUp less the maximum (infinite: none yet), and the lane's sum of weights
+    // kPUp less the maximum (infinite: none yet), and the lane's sum of weights.  Maxima are rounded up to whole numbers:
+    // differences of them, in rescaling and in joining partial results, are then exact powers of two.
+    float base[MT], l[MT];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         base[t] = INFINITY;
@@ -480,7 +484,7 @@ __global__ __launch_bounds__(kThreads, MT == 1 && sizeof(QT) == 2 ? 3 : 2) void 
                 }
                 high = across_groups_max(high);
                 if (high > -INFINITY) {
-                    const float to = fminf(kPUp - high, base[t]);
+                    const float to = fminf(kPUp - ceilf(high), base[t]);
                     const float down = __builtin_amdgcn_exp2f(to - base[t]);      // 0 before the first maximum
                     l[t] *= down;
 #pragma unroll
