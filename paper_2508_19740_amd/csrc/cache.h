@@ -52,7 +52,7 @@ struct DensePlan {
     int64_t about;              // runs of a sequence, on average
     bool splits, joins;         // whether there are partial results, and whether the last workgroup joins them
 };
-int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d);
+int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d, int code_type = SPOTLIGHT_E4M3);
 
 // Whether the last workgroup of each group of rows joins its partial results, instead of a launch of its own: small
 // calls, where the join is one round of loads (about 2 us, since nothing of it is in a cache; a launch takes 3.5 us of the

@@ -651,18 +651,34 @@ void launch_mt(StageTimer& timer, const DenseArgs& a, const DensePlan& d)
 }  // namespace
 
 namespace cache {
-int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d)
+int plan_dense(const Plan& p, int n_cus, int64_t n_tokens, int n_q, const int32_t* lens, DensePlan* d, int code_type)
 {
     const int64_t rows = static_cast<int64_t>(p.G) * n_q;
     if (rows > 1 << 24) return SPOTLIGHT_ERR_UNSUPPORTED;
     DenseShares& s = d->shares;
-    // Two tiles of rows share the reads of codes and their conversion, one has the faster loads.  With one / two, nothing in a
-    // cache, E4M3: 17 rows, 32 MB 20.1 / 21.5 us, 64 MB 27.0 / 30.7, 128 MB 39.5 / 38.3 (integers 39.6 / 37.9); 32 rows, 32 MB
-    // 20.9 / 25.4, 64 MB 27.9 / 33.4, 128 MB 39.2 / 40.6, 256 MB 66.3 / 60.6 (integers 71.9 / 62.7); 64 MB, 48 rows 27.1 / 31.6,
-    // 128 rows 45.2 / 44.3, 512 rows 136 / 108.  Binary32 rows, three parts each, leave no registers for two (512 rows 165 /
-    // 173 us, 17 rows 34.7 / 45.4).
+    // Two tiles of rows a workgroup share the reads of codes and their conversion; one has the faster loads, and shorter work
+    // before and behind the keys.  Up to 32 rows, two pay where the codes are read from memory once and pass the last-level cache by, and
+    // for integers, whose conversion takes twice the instructions, up to 24 rows from 96 MB on; of more rows, whose codes several
+    // workgroups read, where there is enough to do: rows times bytes.  With one / two, us, nothing in a cache, 8 key-value
+    // heads, E4M3:
+    //     MB    17 rows      32 rows      33 rows      64 rows      128 rows     256 rows     1024 rows
+    //      4    13.4 / 14.9  13.4 / 17.4  15.1 / 19.7  15.3 / 19.8  16.6 / 22.1  16.6 / 22.1  21.9 / 23.1
+    //     16    15.3 / 16.7  15.9 / 19.5  18.0 / 21.4  18.1 / 22.1  23.8 / 27.6  35.6 / 39.1  72.9 / 60.5
+    //     32    19.1 / 20.5  19.9 / 21.5  21.4 / 23.2  23.4 / 23.9  30.4 / 29.5  45.7 / 40.9  140 / 117
+    //     64    25.4 / 29.7  26.4 / 32.2  29.6 / 33.4  33.7 / 33.7  48.8 / 45.1  79.1 / 66.7
+    //    128    38.2 / 40.9  38.5 / 42.6  45.8 / 49.3  53.4 / 49.7  84.5 / 73.4  154 / 124
+    //    192    47.6 / 50.0  48.6 / 53.0  61.0 / 60.9  73.0 / 62.9  123 / 102    226 / 180
+    //    256    61.0 / 56.3  61.4 / 60.5  78.9 / 77.7  94.1 / 78.4  162 / 132    297 / 232
+    //    512    111 / 94     111 / 98     143 / 139    173 / 143    310 / 247    582 / 449
+    // Integers, two against one, mean of 10 layouts: 17 rows 64 MB +5 %, 96 MB -1 %, 144 MB -3 %, 208 MB -4 %; 24 rows +8, +2, -1, -2 %; 32
+    // rows +11, +5, +3, 0 %.  E4M3: 17 rows +9, +3, +1, +2 %; 32 rows +16, +10, +7, +5 %.
+    // Over 1418 such cells (1 to 128 heads of sequences and keys, both codes, 1 to 512 MB, 17 to 2048 rows) the rule is 0.5 % behind the faster
+    // kernel on average, in 57 cells by over 5 %, at worst by 18 % (64 MB in 128 heads, 64 rows).  Binary32 rows, three parts each,
+    // leave no registers for two (512 rows 165 / 173 us, 17 rows 34.7 / 45.4).
     const int64_t bytes = 2 * n_tokens * kHeadDim * p.B * p.Hkv;
-    d->row_tiles = rows <= (bytes < kCacheBytes / 2 ? 32 : 16) || p.kv_dtype == SPOTLIGHT_F32 ? 1 : 2;
+    const int64_t few = code_type == SPOTLIGHT_I8 && rows <= 24 ? kCacheBytes / 8 * 3 : kCacheBytes;
+    const bool two = rows > 32 ? rows >= (12 * kCacheBytes + bytes - 1) / bytes : rows > 16 && bytes >= few;
+    d->row_tiles = two && p.kv_dtype == SPOTLIGHT_BF16 ? 2 : 1;
     const int64_t most_rows = 16 * d->row_tiles, tiles = (rows + most_rows - 1) / most_rows, per = tiles * p.Hkv;   // workgroups of a run
     s.lens = lens;
     s.batch = static_cast<uint32_t>(p.B);
@@ -739,7 +755,7 @@ int launch_cache_dense(spotlight_ctx* ctx, const void* q, const spotlight_cache&
     a.negate = scale < 0.0f;
 
     DensePlan d;
-    const int rc = plan_dense(p, ctx->n_cus, n_tokens, n_q, lens, &d);
+    const int rc = plan_dense(p, ctx->n_cus, n_tokens, n_q, lens, &d, c.code_type);
     if (rc != SPOTLIGHT_OK) return rc;
     a.shares = d.shares;
     a.by_queries = fast_div(a.n_q);
