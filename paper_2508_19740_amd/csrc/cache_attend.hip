@@ -238,6 +238,14 @@ void launch_rb(spotlight_ctx* ctx, StageTimer& timer, AttendArgs& a)
     timer.launch(cache_attend_kernel<CT, QT, RB, NT>, dim3(static_cast<unsigned>(a.nsplit), static_cast<unsigned>(p.B * p.Hq)), dim3(NT), 0, a);
 }
 
+// Rows of a workgroup.  Up to 256 rows a head's are in one workgroup of 16 wavefronts, without a merge; then as many a workgroup as leave
+// 1024 workgroups, four a compute unit.  Measured (us, E4M3, caches of which nothing is in a cache; heads x rows: one
+// workgroup a head / 128 / 64 / 32 rows a workgroup, where small grids are joined in place):
+//   1 x 256      7.1 / 10.4 / 10.0 /  7.1      512 x 128   8.9 /  8.1 / 11.8 / 12.7      512 x 256  11.5 / 13.6 / 13.3 / 17.0
+//   1 x 2048       - / 10.1 / 10.1 /  7.1      128 x 512     - / 10.7 / 10.6 / 12.5      512 x 512     - / 18.6 / 18.1 / 27.1
+//  32 x 512        - / 10.3 / 10.8 / 10.7      128 x 2048    - / 18.2 / 18.1 / 26.9      512 x 4096    - / 84.5 / 91.4 / 156
+// At the borders the rule is behind the best choice by up to 18 % (128 x 384 11.7 against 10.2, 1 x 8192 11.3 against 9.7, 8 x 8192
+// 11.9 against 10.9, 512 x 64 8.4 against 7.9).
 template <typename CT, typename QT>
 int launch_t(spotlight_ctx* ctx, AttendArgs& a)
 {
