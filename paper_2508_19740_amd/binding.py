@@ -375,19 +375,24 @@ class Spotlight:
         return cache
 
     def cache_read(self, cache: Cache, n: int, t0: int = 0, first=None, K=None, V=None) -> Tuple[torch.Tensor, torch.Tensor]:
-        """Rows t0 + first[b] .. + n - 1 of the cache as K, V [B, Hkv, n, d] in kv_dtype."""
+        """Rows t0 + first[b] .. + n - 1 of the cache as K, V [B, Hkv, n, d] in kv_dtype, into the tensors given or new
+        ones.  K or V False: that one is not read, and None is returned in its place."""
         self._sync_stream()
         shape = (self.B, self.Hkv, n, self.d)
         # what is made here needs no check; a second tensor like the first takes half the time of one from its shape
-        if K is None:
-            K = torch.empty(shape, dtype=self.kv_dtype, device=self.device) if V is None else torch.empty_like(V)
-        else:
-            self._chk(K, shape, self.kv_dtype, "K")
-        if V is None:
-            V = torch.empty_like(K)
-        else:
-            self._chk(V, shape, self.kv_dtype, "V")
-        rc = lib.spotlight_cache_read(self._h, self._cache(cache), t0, n, self._per_entry(first, "first"), K.data_ptr(), V.data_ptr())
+        made = None
+        out = []
+        for name, x in (("K", K), ("V", V)):
+            if x is None:
+                made = x = torch.empty(shape, dtype=self.kv_dtype, device=self.device) if made is None else torch.empty_like(made)
+            elif x is False:
+                x = None
+            else:
+                self._chk(x, shape, self.kv_dtype, name)
+            out.append(x)
+        K, V = out
+        rc = lib.spotlight_cache_read(self._h, self._cache(cache), t0, n, self._per_entry(first, "first"),
+                                      None if K is None else K.data_ptr(), None if V is None else V.data_ptr())
         if rc != OK:
             raise SpotlightError(rc, "spotlight_cache_read")
         return K, V

@@ -1,5 +1,5 @@
-"""Calls of the 8-bit cache that are large or begin anywhere: writes of more rows than the last-level cache holds over blocks that are
-continued, hashing of rows that lie by themselves at any position and in every size class."""
+"""Calls of the 8-bit cache that are large, begin anywhere, or leave something out: writes of more rows than the last-level cache holds
+over blocks that are continued, hashing of rows that lie by themselves at any position and in every size class, reading K or V alone."""
 import math
 
 import pytest
@@ -83,4 +83,26 @@ def test_hash_rows_at_any_position(b, hkv, n, t0, behind, hidden, bits, kv):
         if e > a:
             ctx.hash_rows(rows[:, :, a:e].contiguous(), *weights, t0 + a, part)
     assert torch.equal(part[:, :, t0:t0 + n], want[:, :, t0:t0 + n])
+    ctx.close()
+
+
+@pytest.mark.parametrize("kv", ["bf16", "f32"])
+def test_reading_keys_or_values_alone(kv):
+    ctx = sp.Spotlight(2, 3, 3, 128, 256, 100, 1, kv_dtype=cc.KV[kv], device=DEV)
+    cache = cc.random_cache(2, 3, 100, 32, "i8", 3).device()
+    K, V = ctx.cache_read(cache, 50, 20)
+    for skip in (0, 1):
+        args = {"K": False} if skip == 0 else {"V": False}
+        got = ctx.cache_read(cache, 50, 20, **args)
+        assert got[skip] is None and torch.equal(got[1 - skip], (K, V)[1 - skip])
+    out = torch.full_like(V, 9.0)
+    k, v = ctx.cache_read(cache, 50, 20, K=False, V=out)
+    assert k is None and v is out and torch.equal(out, V)
+    k, v = ctx.cache_read(cache, 50, 20, V=out.fill_(9.0))
+    assert torch.equal(k, K) and v is out and torch.equal(out, V)
+    with pytest.raises(sp.SpotlightError) as e:
+        ctx.cache_read(cache, 50, 20, K=False, V=False)
+    assert e.value.rc == sp.ERR_INVALID_ARG
+    with pytest.raises(ValueError):
+        ctx.cache_read(cache, 50, 20, K=False, V=out[:, :, :49])
     ctx.close()
