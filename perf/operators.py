@@ -136,8 +136,9 @@ def _cones(g, heads):
 
 
 def _capacity(case):
-    """Tokens the cache has room for: a little more than the case uses, not a multiple of a block."""
-    return (case["first"] + case["rows"] + 5 if case["kind"] == "write" else case["tokens"] + 3)
+    """Tokens the cache has room for: a little more than the case uses, not a multiple of a block; as many as there are queries, which
+    a call asks for (a short cache drawn with more of them was refused)."""
+    return (case["first"] + case["rows"] + 5 if case["kind"] == "write" else max(case["tokens"], case.get("queries", 1)) + 3)
 
 
 def _window(case):
