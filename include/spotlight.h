@@ -344,6 +344,9 @@ int spotlight_sparse_decode_cache(spotlight_ctx *ctx, const void *q, const spotl
  *   q     [B, Hq, n_q, d]  kv_dtype
  *   lens  [B]              int32, device, or NULL
  *   out   [B, Hq, n_q, d]  float32
+ * Weights enter the sums of values with 22 bits, and down to 2^-31 of the largest weight among the keys they are summed with: those of
+ * a run of keys whose value scales lie within 2^12 of each other, else those among 16 tokens.  What a query does not attend, or
+ * weighs 0, has no part in its result, whatever its values.
  * The call enqueues two kernels, or one where the keys need no splitting and in small calls, and nothing else.
  * Errors: INVALID_ARG for a bad cache, a misaligned q (16 bytes) or unless 1 <= n_tokens <= Nmax and 1 <= n_q <= Nmax;
  * UNSUPPORTED for more than 2^24 / (Hq / Hkv) queries, for 2^24 or more tiles of 32 rows (16 in binary32) of B x Hkv x (Hq / Hkv) n_q, or if
@@ -370,7 +373,8 @@ int spotlight_hash_rows(spotlight_ctx *ctx, const void *K, const spotlight_hash_
  *   q      [B, Hq, d]         kv_dtype
  *   K, V   [B, Hkv, 1, d]     kv_dtype   the new token's rows
  *   codes, out_idx, out       as for spotlight_decode_step
- * Six kernels at most and nothing else, so the call can be captured into a HIP graph.
+ * Six kernels at most, seven where hidden is not a multiple of 128, and nothing else, so the call can be captured into a HIP
+ * graph.
  * Errors: those of spotlight_decode_step; INVALID_ARG for a bad cache.
  */
 int spotlight_decode_step_cache(spotlight_ctx *ctx, const void *q, const void *K, const void *V, const spotlight_cache *cache,

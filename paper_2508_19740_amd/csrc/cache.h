@@ -40,7 +40,7 @@ struct DenseShares {
     uint32_t batch, units;      // units of n_tokens
     uint32_t chunk;             // units of a run, and
     uint32_t nsplit;            // runs of a sequence, without lens
-    uint32_t most_runs;         // with lens: runs of all sequences, at least twice as many as there are sequences; 0: a run is a sequence
+    uint32_t most_runs;         // with lens: runs of all sequences, more than there are sequences (twice as many where there is room); 0: a run is a sequence
     uint32_t tile_rows;         // rows of a workgroup's partial result
     uint32_t tiles;             // tiles of rows of a key-value head
     FastDiv by_nsplit, by_most, by_spare, by_heads, by_tiles8;    // by_spare: most_runs - batch

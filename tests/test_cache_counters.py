@@ -158,12 +158,15 @@ int main()
                     Plan p;
                     if (make_plan(&cfg, &p) != SPOTLIGHT_OK) return 2;
                     std::vector<cache::DensePlan> plans;
-                    for (int nq : {1, 2, 17, 128, 300})
+                    for (int nq : {1, 2, 17, 128, 300, 4096})
                         for (int ragged : {0, 1}) {
                             cache::DensePlan d;
                             int32_t one;
-                            if (cache::plan_dense(p, 256, n, nq, ragged ? &one : nullptr, &d) == SPOTLIGHT_OK && d.splits) plans.push_back(d);
+                            if (nq <= n && cache::plan_dense(p, 256, n, nq, ragged ? &one : nullptr, &d) == SPOTLIGHT_OK && d.splits) plans.push_back(d);
                         }
+                    // sequences of lengths of their own: a run each and at least one to spare, by which the kernel divides
+                    for (const auto& d : plans)
+                        if (d.shares.most_runs && (d.shares.most_runs <= static_cast<uint32_t>(B) || d.shares.by_spare.d != d.shares.most_runs - B)) return 6;
                     for (const auto& mine : plans)
                         for (const auto& table : plans) {
                             cache::MergeRows r = {};
