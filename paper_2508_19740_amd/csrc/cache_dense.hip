@@ -29,9 +29,11 @@
 //
 // Where the scales of a run's values lie further apart than 2^12 (a key of huge values, or a block of zeros, whose scale
 // is the least there is), or one is NaN, a row must not lose the small values that it attends to a large one that it does not
-// see, or weighs 0.  There, the 16 keys of a block have products of their own (v_mfma_f32_16x16x16_f16), with weights relative to the row's
-// largest among them, and meet the others in binary32 with that weight and the block's scale: 64 more multiply-adds a tile.  (2^12: what the second part of p drops, 2^-32 of the largest weight, is then 2^-20 of the least
-// block's values at most.)
+// see, or weighs 0.  There, the 16 keys of a block have products of their own (v_mfma_f32_16x16x16_f16), with weights
+// relative to the row's largest among them, and meet the others in binary32 with that weight and the block's scale: 64 more
+// multiply-adds a tile.  (All runs so: 268 MB, 32 / 8 heads, 48.1 -> 53.4 us, 128 queries over 67 MB 122 -> 195 us; other runs lose
+// nothing.  2^12: what the second part of p drops, 2^-32 of the largest weight, is then 2^-20 of the least block's
+// values at most.)
 //
 // A row reads 256 bytes a key and key-value head, whatever G and n_q: with few rows the kernel is bound by
 // memory.  The keys are split over workgroups, and a merge joins them.
