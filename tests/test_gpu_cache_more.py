@@ -106,3 +106,44 @@ def test_reading_keys_or_values_alone(kv):
     with pytest.raises(ValueError):
         ctx.cache_read(cache, 50, 20, K=False, V=out[:, :, :49])
     ctx.close()
+
+
+def test_two_graphs_and_eager_calls_on_one_context():
+    """Small calls of different group sizes, whose last workgroups join the parts, captured into two graphs that share a context's
+    workspace and counters, replayed in turn with eager calls of other sizes between: every result is the eager one."""
+    n = 4000
+    host = cc.random_cache(2, 2, n, 64, "e4m3", 17)
+    ctx, cache = sp.Spotlight(2, 4, 2, 128, 256, n, 600, device=DEV), host.device()
+    g = torch.Generator().manual_seed(3)
+    q = torch.randn(2, 4, 1, cc.D, generator=g).to(torch.bfloat16).to(DEV)
+    lens = torch.tensor([n, 700], dtype=torch.int32, device=DEV)
+    idx = torch.randint(0, n, (2, 4, 600), generator=g, dtype=torch.int32).to(DEV)
+    calls = [lambda: ctx.dense_decode_cache(q, cache, n, lens), lambda: ctx.sparse_decode_cache(q[:, :, 0], cache, idx[:, :, :500].contiguous()),
+             lambda: ctx.dense_decode_cache(q, cache, 1500), lambda: ctx.sparse_decode_cache(q[:, :, 0], cache, idx),
+             lambda: ctx.dense_decode_cache(q, cache, n)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for c in calls:
+            c()
+    side.synchronize()
+    want = [c().clone() for c in calls]
+    torch.cuda.synchronize()
+    graphs = []
+    for pick in ((0, 1), (2, 3, 0)):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = [calls[i]() for i in pick]
+        graphs.append((graph, pick, out))
+    for r in range(12):
+        graph, pick, out = graphs[r % 2]
+        for o in out:
+            o.fill_(math.nan)
+        graph.replay()
+        e = calls[r % 5]()
+        assert torch.equal(e, want[r % 5])
+        for i, o in zip(pick, out):
+            assert torch.equal(o, want[i]), (r, i)
+        if r % 3 == 0:
+            torch.cuda.synchronize()
+    ctx.close()
